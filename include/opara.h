@@ -58,6 +58,7 @@ enum opara_status {
 enum opara_op_type {
   OPARA_CONV2D = 0, OPARA_GEMM, OPARA_BGEMM, OPARA_MAXPOOL, OPARA_AVGPOOL, OPARA_GAVGPOOL,
   OPARA_CONCAT, OPARA_LAYERNORM, OPARA_SOFTMAX, OPARA_GELU, OPARA_RELU, OPARA_ADD,
+  OPARA_ROTARY, OPARA_RESIDUAL_NORM, OPARA_GATED, OPARA_ATTENTION,   /* the blocks of a decoder */
   OPARA_N_OP_TYPES
 };
 
@@ -69,7 +70,23 @@ enum opara_mode  { OPARA_PARALLEL = 0, OPARA_SEQUENTIAL = 1, OPARA_PARALLEL_CAPT
 
 enum opara_flags {
   OPARA_FLAG_RELU     = 1u,  /* CONV2D / GEMM: clamp the result at zero                    */
-  OPARA_FLAG_B_KMAJOR = 2u   /* BGEMM: second operand stored [K][N] (N fastest), else [N][K] */
+  OPARA_FLAG_B_KMAJOR = 2u,  /* BGEMM: second operand stored [K][N] (N fastest), else [N][K] */
+  OPARA_FLAG_INTERLEAVED = 4u, /* ROTARY: a pair is (2i, 2i+1), else (i, i + rotated/2)    */
+  OPARA_FLAG_CAUSAL = 8u,    /* ATTENTION: query row i sees key rows j <= i + first        */
+  OPARA_FLAG_CAUSAL_END = 16u, /* ATTENTION: ... j <= i + (rows of the sequence) - m       */
+  OPARA_FLAG_NORM_AFTER = 32u, /* RESIDUAL_NORM: norm of inputs[0] before it is added      */
+  OPARA_FLAG_NORM_BEFORE = 64u, /* RESIDUAL_NORM: norm of the sum (the next block's)       */
+  OPARA_FLAG_RMS = 128u      /* RESIDUAL_NORM: divide by the root mean square, keep the mean */
+};
+
+/* What GATED applies to its gate. */
+enum opara_activation {
+  OPARA_ACT_SILU = 0,        /* x / (1 + exp(-x))                                          */
+  OPARA_ACT_GELU = 1,        /* exact erf form                                             */
+  OPARA_ACT_GELU_TANH = 2,   /* 0.5 x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3)))            */
+  OPARA_ACT_RELU = 3,
+  OPARA_ACT_SIGMOID = 4,
+  OPARA_N_ACTIVATIONS
 };
 
 /* Per-compute-unit limits that turn a demand record into one integer
@@ -100,6 +117,37 @@ typedef struct {
  *   LAYERNORM/SOFTMAX m rows, n cols, eps (LayerNorm: biased variance, gamma 1, beta 0),
  *                     applied to the SUM of all inputs, each viewed [m][n].
  *   GELU/RELU/ADD     m*n elements; f(sum of all inputs).  GELU is the exact erf form.
+ *   ROTARY            m rows of heads heads of width elements (1..4096); the first `rotated` elements
+ *                     of every head (even, 2..width) are taken in pairs (u, v) and rotated by
+ *                     the angle of the row's position p and the pair i,
+ *                       (u, v) -> alpha * (u cos - v sin, v cos + u sin),  angle = 2 pi frac(p * weight[i] / 2^64),
+ *                     the others are copied.  weight: device uint64[rotated / 2], from
+ *                     opara_rotary_table or the caller's own.  p = inputs[1][row] (device int32[m], any
+ *                     value) or, without that input, first + row.  a_row_stride / c_row_stride
+ *                     (0 = heads * width): elements between rows of the input / the result.
+ *   RESIDUAL_NORM     m rows, n columns.  z = inputs[0], normalised with NORM_AFTER, times the gate
+ *                     (inputs[2], [batch][n], 0 = m rows of it; row r takes gate row r / (m / batch),
+ *                     m a multiple of batch); s = alpha * inputs[1] + beta * z (beta * z without a second
+ *                     input).  out = s or, with NORM_BEFORE, the norm of s, and out2, unless it is
+ *                     null, s.  norm(x) = (x - mean) / sqrt(var + eps) * w + b, with RMS
+ *                     x / sqrt(mean of squares + eps) * w + b.  weight: [n] elements per norm that is asked
+ *                     for, NORM_AFTER's first, null = ones; bias likewise, fp32, null = zeros.
+ *   GATED             m,n,k, activation: Y[m][n] = act(X.Wg + bg) * (X.Wu + bu); weight [2n][k]: n rows
+ *                     Wg, then n rows Wu; bias fp32 [2n], bg then bu.  a_row_stride (0 = k), c_row_stride
+ *                     (0 = n): elements between rows of the input / the result.
+ *   ATTENTION         batch (0 = 1) sequences, heads query heads that share kv_heads (0 = heads; a
+ *                     divisor of heads) key and value heads in runs of heads / kv_heads, m query rows,
+ *                     n key rows, width (1..256) elements of a query or key, v_width (0 = width; 1..256) of a value.
+ *                     Y[b][i][h] = softmax over the visible j of (alpha Q[b][i][h] . K[b][j][g]) . V[b][j][g].
+ *                     inputs: Q, K, V and optionally int32[batch], the valid key rows of every sequence
+ *                     (below 0 counts as 0, above n as n; without it n).  CAUSAL, CAUSAL_END: see
+ *                     opara_flags.  A query row that sees no key gives zeros.  Key and value rows behind
+ *                     a sequence's length, and those behind the last one that a query row of it sees,
+ *                     are not used, whatever they hold; inside, a value row that some query rows see must be finite
+ *                     for the others to be.  strides: elements between sequences, rows and heads of
+ *                     Q, K, V and Y; a triple of zeros = packed [batch][rows][heads][width].
+ *                     scratch: see opara_scratch_bytes.
+ * heads ... beta, strides, out2 and scratch are fields of opara_op_more.
  * Every input is read as the leading prefix of its producer's buffer in the shape above.
  */
 typedef struct {
@@ -120,7 +168,8 @@ typedef struct {
 typedef struct {
   int32_t  op_type;                    /* enum opara_op_type                                */
   int32_t  op_class;                   /* enum opara_class; DEFAULT = by op_type: CONV2D,
-                                          GEMM, BGEMM are COMP, everything else MEM         */
+                                          GEMM, BGEMM, GATED, ATTENTION are COMP, everything
+                                          else MEM                                          */
   int32_t  dtype;                      /* enum opara_dtype                                  */
   int32_t  n_inputs;                   /* 1..OPARA_MAX_INPUTS                               */
   int32_t  inputs[OPARA_MAX_INPUTS];   /* producer operator ids in ARGUMENT ORDER;
@@ -141,6 +190,20 @@ typedef struct {
                                           arguments in the predecessor order.               */
 } opara_op_desc;
 
+/* What ROTARY, RESIDUAL_NORM, GATED and ATTENTION state beyond an opara_op_desc, and which results any
+ * operator reads; one per operator beside the descriptors (opara_build_dag_more).  All zeros otherwise. */
+typedef struct {
+  int32_t heads, kv_heads, width, v_width, rotated, first, activation;
+  float   beta;
+  int64_t strides[4][3];               /* ATTENTION: Q, K, V, Y x sequence, row, head      */
+  void *out2;                          /* device, caller-owned: RESIDUAL_NORM's second result, may be
+                                          NULL; others: NULL                                */
+  int32_t  result_of[OPARA_MAX_INPUTS]; /* inputs[i] is its producer's out (0) or out2 (1)  */
+  void *scratch;                       /* device, caller-owned, 256-byte aligned, may be NULL: see
+                                          opara_scratch_bytes                               */
+  uint64_t scratch_bytes;
+} opara_op_more;
+
 /* What opara_get_demands reports per operator. */
 typedef struct {
   uint32_t grid_blocks, block_threads, lds_bytes, vgprs;
@@ -160,6 +223,41 @@ typedef struct {
 int opara_build_dag(const opara_op_desc *ops, int32_t n_ops,
                     void *const *ext_inputs, int32_t n_ext,
                     const opara_limits *lim, opara_dag **out);
+
+/*
+ * The same for a list with operators that need an opara_op_more: more[i] goes with ops[i] (copied, like
+ * them).  more == NULL is opara_build_dag, which refuses ROTARY, RESIDUAL_NORM, GATED and ATTENTION (EINVAL).  After
+ * opara_elide_concats the record of operator v belongs beside new_id[v], as it is.
+ */
+int opara_build_dag_more(const opara_op_desc *ops, const opara_op_more *more, int32_t n_ops,
+                         void *const *ext_inputs, int32_t n_ext,
+                         const opara_limits *lim, opara_dag **out);
+
+/*
+ * Frequencies of ROTARY as fractions of a turn per position, in units of 2^-64: what the
+ * operator takes as its weight.  turns: host uint64[rotated / 2] (the caller uploads it).
+ * Pair i turns base^(-2i/rotated) radians per position.  For contexts longer than the trained one
+ * every frequency is divided by `factor` (1 = as trained); with original_length > 0 only the slow
+ * ones: a pair that makes at least `high` turns within original_length keeps its frequency, one
+ * that makes at most `low` has it divided, and between them the two are mixed in proportion.
+ * The phase of a position is its product with the frequency modulo one turn, which integers of 64
+ * bits give without the rounding that fp32 angles of far positions suffer (at position 2^20
+ * the error is below 2^-44 turns).  No HIP call.  Errors: EINVAL (rotated not even or outside 2..4096, base or
+ * factor not positive and finite, original_length negative, low >= high).
+ */
+int opara_rotary_table(int32_t rotated, double base, double factor, double original_length, double low, double high,
+                       uint64_t *turns);
+
+/*
+ * Scratch memory an operator can use (0 for all but ATTENTION).  ATTENTION over many keys with
+ * few query rows shares the keys out between workgroups and joins their results; for that it
+ * needs this much device memory, which must hold zeros when the operator first runs and is left so that it
+ * can run again.  It belongs to this operator alone; executors of one DAG share it like they share its
+ * result buffers, so their replays must not overlap.  Without scratch, or with less than this, one
+ * workgroup walks all keys of its query rows.  Looks at op_type, dtype, params and more's shape (more may be NULL
+ * where the operator needs none).  No HIP call.  Errors: as opara_build_dag.
+ */
+int opara_scratch_bytes(const opara_op_desc *op, const opara_op_more *more, uint64_t *bytes);
 
 /*
  * Zero-copy concatenation, a rewrite of the operator list applied before opara_build_dag
@@ -409,7 +507,8 @@ int opara_verify_dependencies(opara_dag *g, void *hip_stream, int32_t *n_violati
  * assumption is residency: work items are dealt to workgroups statically, so the launch
  * makes progress only while all its workgroups are resident; co-running kernels that hold
  * compute units for long can make a wait run out (reported, see below).
- * Errors: ESTATE without a launch queue, EINVAL (workspace), EUNSUPPORTED (more than 8
+ * Errors: ESTATE without a launch queue, EINVAL (workspace), EUNSUPPORTED (a ROTARY, RESIDUAL_NORM,
+ * GATED or ATTENTION operator behind the serial prefix: their kernels are launches of their own; more than 8
  * predecessors or 65535 tiles per operator, more than about 2,600 operators, mixed
  * element types), EHIP.
  * Replay with opara_replay, destroy with opara_exec_destroy.
@@ -515,7 +614,8 @@ int opara_run_persistent_noalloc(opara_dag *g, void *hip_stream, uint32_t *error
  * a node of its own, which launches nothing: opara_fused_time_nodes reports 0 for it and opara_exec_info does not
  * count it.  Executors captured with the operator timeline on run every operator by itself.
  */
-enum { OPARA_GROUP_KERNEL_LIGHT = -1, OPARA_GROUP_KERNEL_HEAVY = -2, OPARA_GROUP_KERNEL_STREAM = -3 };
+enum { OPARA_GROUP_KERNEL_LIGHT = -1, OPARA_GROUP_KERNEL_HEAVY = -2, OPARA_GROUP_KERNEL_STREAM = -3,
+       OPARA_GROUP_KERNEL_DECODER = -4 };   /* ROTARY and RESIDUAL_NORM operators of a wave */
 int opara_fused_plan(const opara_exec *e, int32_t *node_of, int32_t *n_nodes, int32_t *node_kernel);
 /*
  * Measurement aid: launches every node of a fused executor by itself (an ordinary launch

@@ -87,12 +87,26 @@ def run_op(op, ins, wts):
         return O.relu(ins)
     if t == "add":
         return O.add(ins)
+    if t == "rotary":
+        positions = ins[1] if len(ins) > 1 else p["first"] + np.arange(ins[0].shape[0])
+        return O.rotary(ins[0], p["heads"], p["width"], p["rotated"], p["interleaved"], positions, p["base"], p["factor"],
+                        p["original"], p["low"], p["high"], p["alpha"])
+    if t == "residual_norm":
+        f64 = lambda a: None if a is None else np.asarray(a, dtype=np.float64)
+        wts = wts or {"w": None, "b": None}
+        return O.residual_norm(ins[0], ins[1] if len(ins) > 1 else None, ins[2] if len(ins) > 2 else None, f64(wts["w"]), f64(wts["b"]),
+                               p["rms"], p["after"], p["before"], p["alpha"], p["beta"], p["eps"])
+    if t == "gated":
+        return O.gated(ins[0], wts["w"].astype(np.float64), wts["b"].astype(np.float64), p["activation"])
+    if t == "attention":
+        return O.attention(ins[0], ins[1], ins[2], p["batch"], p["heads"], p["kv_heads"], p["width"], p["v_width"], p["alpha"],
+                           ins[3] if len(ins) > 3 else None, p["causal"], p["first"])
     raise ValueError(f"unknown operator type {t}")
 
 
 def run_dag(wl, order=None, keep=None):
-    """Execute workload `wl`; returns {op id: output rounded to wl dtype (as stored)}.
-    keep: iterable of op ids whose outputs to return (default: all)."""
+    """Execute workload `wl`; returns {op id: output rounded to wl dtype (as stored)}; an operator's second result
+    is under (op id, 1).  keep: iterable of op ids whose outputs to return (default: all)."""
     n = len(wl.ops)
     order = kahn_order(n, wl.edges()) if order is None else list(order)
     st = wl.np_dtype
@@ -102,19 +116,23 @@ def run_dag(wl, order=None, keep=None):
             if u >= 0:
                 remaining[u] += 1
     keep = set(range(n)) if keep is None else set(keep)
-    out = {}
+    out, second = {}, {}
     for v in order:
         op = wl.ops[v]
         batched = wl.batch > 1 and is_image_op(op)     # image operators act on each image alone
         ins = []
-        for u, shp in zip(op.inputs, op.in_shapes):
-            src = wl.ext_inputs[-u - 1] if u < 0 else out[u]
+        for i, (u, shp) in enumerate(zip(op.inputs, op.in_shapes)):
+            src = wl.ext_inputs[-u - 1] if u < 0 else second[u] if i in op.second else out[u]
             ins.append(_view(src, ((wl.batch,) + tuple(shp)) if batched else shp).astype(np.float64))
         if batched:
             y = np.stack([run_op(op, [a[b] for a in ins], wl.weights.get(v)) for b in range(wl.batch)])
             assert y.shape[1:] == tuple(op.out_shape), (op.name, y.shape, op.out_shape)
         else:
             y = run_op(op, ins, wl.weights.get(v))
+            if isinstance(y, tuple):
+                y, s = y
+                if s is not None:
+                    second[v] = s.astype(st)
             assert y.shape == tuple(op.out_shape), (op.name, y.shape, op.out_shape)
         out[v] = y.astype(st)
         for u in op.inputs:
@@ -122,4 +140,5 @@ def run_dag(wl, order=None, keep=None):
                 remaining[u] -= 1
                 if remaining[u] == 0 and u not in keep:
                     del out[u]
-    return {v: a for v, a in out.items() if v in keep}
+                    second.pop(u, None)
+    return {**{v: a for v, a in out.items() if v in keep}, **{(v, 1): a for v, a in second.items() if v in keep}}

@@ -138,3 +138,71 @@ def relu(xs):
 
 def add(xs):
     return _sum(xs)
+
+
+def rotary(x, heads, width, rotated, interleaved, positions, base, factor, original, low, high, alpha=1.0):
+    """Every head's first `rotated` columns in pairs, as complex numbers, times alpha * exp(i p f_j): pair j is
+    (2j, 2j+1) or (j, j + rotated/2), f_j = base^(-2j/rotated) radians per position.  Stretched for
+    long contexts: f_j / factor; with original > 0 only for pairs that turn less than `low` times within
+    `original` positions, unchanged from `high` turns on, mixed linearly in the number of turns between."""
+    m = x.shape[0]
+    j = np.arange(rotated // 2)
+    f = np.power(float(base), -2.0 * j / rotated)
+    if original > 0:
+        turns = original * f / (2.0 * np.pi)
+        keep = np.clip((turns - low) / (high - low), 0.0, 1.0)
+        f = keep * f + (1.0 - keep) * f / factor
+    else:
+        f = f / factor
+    z = alpha * np.exp(1j * np.asarray(positions, dtype=np.float64)[:, None] * f[None, :])[:, None, :]
+    y = x.reshape(m, heads, width).copy()
+    a, b = (slice(0, rotated, 2), slice(1, rotated, 2)) if interleaved else (slice(0, rotated // 2), slice(rotated // 2, rotated))
+    c = (y[..., a] + 1j * y[..., b]) * z
+    y[..., a], y[..., b] = c.real, c.imag
+    return y.reshape(m, heads * width)
+
+
+def residual_norm(x, residual, gate, w, b, rms, after, before, alpha, beta, eps):
+    """(result, sum or None).  z = x or its norm; s = alpha * residual + beta * gate * z, a gate row serving
+    rows / gates rows in turn; the result is the norm of s (the sum beside it) or s.  w, b: a row per norm."""
+    def norm(t, i):
+        if not rms:
+            t = t - t.mean(axis=-1, keepdims=True)
+        t = t / np.sqrt((t * t).mean(axis=-1, keepdims=True) + eps)
+        return t * (1.0 if w is None else w[i]) + (0.0 if b is None else b[i])
+    z = norm(x, 0) if after else x
+    if gate is not None:
+        z = z * np.repeat(gate, x.shape[0] // gate.shape[0], axis=0)
+    s = beta * z + (0.0 if residual is None else alpha * residual)
+    return (norm(s, int(after)), s) if before else (s, None)
+
+
+def gated(x, w, b, activation):
+    """activation(X.Wg + bg) * (X.Wu + bu); w [K, 2N], gate columns first."""
+    g, u = np.split(x @ w + b[None, :], 2, axis=1)
+    act = {"silu": lambda t: t / (1.0 + np.exp(-t)), "gelu": lambda t: 0.5 * t * (1.0 + erf(t / np.sqrt(2.0))),
+           "gelu_tanh": lambda t: 0.5 * t * (1.0 + np.tanh(np.sqrt(2.0 / np.pi) * (t + 0.044715 * t ** 3))),
+           "relu": lambda t: np.maximum(t, 0.0), "sigmoid": lambda t: 1.0 / (1.0 + np.exp(-t))}[activation]
+    return act(g) * u
+
+
+def attention(q, k, v, batch, heads, kv_heads, width, v_width, alpha, lengths=None, causal=None, first=0):
+    """Softmax of alpha Q.K^T over the visible keys, times V, head by head; a run of heads / kv_heads query heads
+    shares a key head.  A query row sees the first `lengths[b]` keys, of these, causal "start", the first
+    i + first + 1 and, causal "end", the first i + lengths[b] - m + 1; one that sees none gives zeros."""
+    m, n = q.shape[0] // batch, k.shape[0] // batch
+    y = np.zeros((batch * m, heads * v_width))
+    for b in range(batch):
+        length = n if lengths is None else int(min(max(lengths[b], 0), n))
+        for h in range(heads):
+            g = h // (heads // kv_heads)
+            kb = k[b * n:b * n + length, g * width:(g + 1) * width]
+            vb = v[b * n:b * n + length, g * v_width:(g + 1) * v_width]
+            for i in range(m):
+                seen = length if causal is None else min(length, i + 1 + (first if causal == "start" else length - m))
+                if seen <= 0:
+                    continue
+                s = alpha * (kb[:seen] @ q[b * m + i, h * width:(h + 1) * width])
+                e = np.exp(s - s.max())
+                y[b * m + i, h * v_width:(h + 1) * v_width] = (e @ vb[:seen]) / e.sum()
+    return y

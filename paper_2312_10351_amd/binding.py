@@ -9,15 +9,18 @@ MAX_INPUTS = 8
 OK, EINVAL, ECYCLE, ENOMEM, ESTATE, EHIP, EUNSUPPORTED, EGRAPH = 0, -1, -2, -3, -4, -5, -6, -7
 NOT_VALIDATED, SCREENED_ON_TWIN, VALIDATED_IN_PLACE = 0, 1, 2
 (CONV2D, GEMM, BGEMM, MAXPOOL, AVGPOOL, GAVGPOOL, CONCAT, LAYERNORM, SOFTMAX, GELU, RELU,
- ADD) = range(12)
+ ADD, ROTARY, RESIDUAL_NORM, GATED, ATTENTION) = range(16)
 OP_TYPE_IDS = dict(conv2d=CONV2D, gemm=GEMM, bgemm=BGEMM, maxpool=MAXPOOL, avgpool=AVGPOOL,
                    gavgpool=GAVGPOOL, concat=CONCAT, layernorm=LAYERNORM, softmax=SOFTMAX,
-                   gelu=GELU, relu=RELU, add=ADD)
+                   gelu=GELU, relu=RELU, add=ADD, rotary=ROTARY, residual_norm=RESIDUAL_NORM,
+                   gated=GATED, attention=ATTENTION)
 CLASS_DEFAULT, MEM, COMP = -1, 0, 1
 F32, F16 = 0, 1
 PARALLEL, SEQUENTIAL, PARALLEL_CAPTURE, PARALLEL_PRUNED, FUSED = 0, 1, 2, 3, 4
 STREAMS_ALG1, STREAMS_MIN = 0, 1
 FLAG_RELU, FLAG_B_KMAJOR = 1, 2
+FLAG_INTERLEAVED, FLAG_CAUSAL, FLAG_CAUSAL_END, FLAG_NORM_AFTER, FLAG_NORM_BEFORE, FLAG_RMS = 4, 8, 16, 32, 64, 128
+ACTIVATION_IDS = dict(silu=0, gelu=1, gelu_tanh=2, relu=3, sigmoid=4)
 (ORDER_ALG2, ORDER_ALG2_COMP_FIRST, ORDER_LEAST_DEMAND, ORDER_MOST_DEMAND, ORDER_TOPO,
  ORDER_LEVEL) = range(6)
 ORDER_POLICY_NAMES = ("alg2", "alg2_comp_first", "least_demand", "most_demand", "topo", "level")
@@ -57,13 +60,20 @@ class OpDesc(C.Structure):
                 ("n_deps", C.c_int32), ("deps", C.c_int32 * MAX_INPUTS)]
 
 
+class OpMore(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("kv_heads", C.c_int32), ("width", C.c_int32), ("v_width", C.c_int32),
+                ("rotated", C.c_int32), ("first", C.c_int32), ("activation", C.c_int32), ("beta", C.c_float),
+                ("strides", (C.c_int64 * 3) * 4), ("out2", C.c_void_p), ("result_of", C.c_int32 * MAX_INPUTS),
+                ("scratch", C.c_void_p), ("scratch_bytes", C.c_uint64)]
+
+
 class Demand(C.Structure):
     _fields_ = [("grid_blocks", C.c_uint32), ("block_threads", C.c_uint32),
                 ("lds_bytes", C.c_uint32), ("vgprs", C.c_uint32),
                 ("op_class", C.c_int32), ("kernel_id", C.c_int32), ("demand", C.c_uint64)]
 
 
-EXPORTS = ["opara_build_dag", "opara_elide_concats", "opara_assign_streams", "opara_assign_streams_policy", "opara_order_launch",
+EXPORTS = ["opara_build_dag", "opara_build_dag_more", "opara_elide_concats", "opara_rotary_table", "opara_scratch_bytes", "opara_assign_streams", "opara_assign_streams_policy", "opara_order_launch",
            "opara_order_launch_policy", "opara_sync_edges", "opara_sync_edges_pruned",
            "opara_get_demands", "opara_wave_of", "opara_topo_order", "opara_num_ops", "opara_capture",
            "opara_persistent_workspace_bytes", "opara_capture_persistent", "opara_persistent_status",
@@ -89,8 +99,12 @@ def load():
     vp, i32p = C.c_void_p, C.POINTER(C.c_int32)
     lib.opara_build_dag.argtypes = [C.POINTER(OpDesc), C.c_int32, C.POINTER(C.c_void_p), C.c_int32,
                                     C.POINTER(Limits), C.POINTER(vp)]
+    lib.opara_build_dag_more.argtypes = [C.POINTER(OpDesc), C.POINTER(OpMore), C.c_int32, C.POINTER(C.c_void_p), C.c_int32,
+                                         C.POINTER(Limits), C.POINTER(vp)]
     lib.opara_elide_concats.argtypes = [C.POINTER(OpDesc), C.c_int32, C.POINTER(C.c_void_p), C.c_int32,
                                         C.POINTER(OpDesc), i32p, i32p, C.POINTER(C.c_void_p), i32p]
+    lib.opara_rotary_table.argtypes = [C.c_int32] + [C.c_double] * 5 + [C.POINTER(C.c_uint64)]
+    lib.opara_scratch_bytes.argtypes = [C.POINTER(OpDesc), C.POINTER(OpMore), C.POINTER(C.c_uint64)]
     lib.opara_assign_streams.argtypes = [vp, i32p, i32p]
     lib.opara_assign_streams_policy.argtypes = [vp, C.c_int32, i32p, i32p]
     lib.opara_sync_edges_pruned.argtypes = [vp, i32p, C.c_int32, i32p]
@@ -155,6 +169,19 @@ def opara_build_dag(descs, ext_ptrs, limits=None):
     return out
 
 
+def opara_build_dag_more(descs, more, ext_ptrs, limits=None):
+    """As opara_build_dag, with an OpMore record beside every descriptor."""
+    if len(more) != len(descs):
+        raise ValueError(f"{len(descs)} descriptors, {len(more)} OpMore records")
+    arr = (OpDesc * max(len(descs), 1))(*descs)
+    beside = (OpMore * max(len(more), 1))(*more)
+    ext = (C.c_void_p * max(len(ext_ptrs), 1))(*ext_ptrs)
+    out = C.c_void_p()
+    lim = C.byref(limits) if limits is not None else None
+    _check(load().opara_build_dag_more(arr, beside, len(descs), ext, len(ext_ptrs), lim, C.byref(out)))
+    return out
+
+
 def opara_elide_concats(descs, ext_ptrs):
     """Zero-copy concatenation rewrite.  Returns (reduced descs, new_id per operator (-1 = removed),
     external pointers of the reduced list)."""
@@ -173,6 +200,20 @@ def opara_elide_concats(descs, ext_ptrs):
         C.memmove(C.byref(d), C.byref(out[i]), C.sizeof(OpDesc))
         reduced.append(d)
     return reduced, list(new_id)[:n], [ext_out[i] or 0 for i in range(n_ext_out.value)]
+
+
+def opara_rotary_table(rotated, base=10000.0, factor=1.0, original_length=0.0, low=1.0, high=4.0):
+    """Frequencies of a rotary operator (its weight) as a list of rotated / 2 integers, 2^-64 turns per position."""
+    t = (C.c_uint64 * max(rotated // 2, 1))()
+    _check(load().opara_rotary_table(rotated, base, factor, original_length, low, high, t))
+    return list(t)
+
+
+def opara_scratch_bytes(desc, more):
+    """Scratch memory the operator can use; `more` may be None where it needs no such record."""
+    n = C.c_uint64()
+    _check(load().opara_scratch_bytes(C.byref(desc), None if more is None else C.byref(more), C.byref(n)))
+    return n.value
 
 
 def opara_num_ops(dag):
@@ -337,7 +378,7 @@ def opara_exec_info(exe):
     return a.value, b.value
 
 
-GROUP_KERNEL_LIGHT, GROUP_KERNEL_HEAVY, GROUP_KERNEL_STREAM = -1, -2, -3
+GROUP_KERNEL_LIGHT, GROUP_KERNEL_HEAVY, GROUP_KERNEL_STREAM, GROUP_KERNEL_DECODER = -1, -2, -3, -4
 
 
 def opara_fused_plan(exe, n_ops):
@@ -353,7 +394,8 @@ def opara_fused_node_kernels(exe, dtype):
     _check(load().opara_fused_plan(exe, None, C.byref(n), None))
     k = (C.c_int32 * n.value)()
     _check(load().opara_fused_plan(exe, None, None, k))
-    group = {GROUP_KERNEL_LIGHT: "light", GROUP_KERNEL_HEAVY: "heavy", GROUP_KERNEL_STREAM: "stream"}
+    group = {GROUP_KERNEL_LIGHT: "light", GROUP_KERNEL_HEAVY: "heavy", GROUP_KERNEL_STREAM: "stream",
+             GROUP_KERNEL_DECODER: "decoder"}
     return [f"group_{dtype}_{group[i]}" if i in group else opara_kernel_info(i)[0] for i in k]
 
 

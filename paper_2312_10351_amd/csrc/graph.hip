@@ -32,7 +32,7 @@ struct opara_exec {
   // fused executor only: the chain of nodes (single operators and groups) and where each operator went
   struct FusedNode {
     bool is_group = false, f16 = false;
-    int flavor = 0;                      // group kernel flavour: 0 stream, 1 light, 2 heavy
+    int flavor = 0;                      // group kernel flavour: 0 stream, 1 light, 2 heavy, kGroupDecoder
     opara::KernelPlan plan;              // single operator, or the first of several that share a kernel
     bool launches = true;                // false: computed by the kernel of an earlier node
     uint32_t blocks = 0, lds = 0;
@@ -259,6 +259,25 @@ int capture_fused(opara_dag *g, opara_exec **out) {
       members.clear();
     };
     int64_t blocks = 0;
+    // A decoder's row-wise operators (the rotations of queries and keys, say) form groups of
+    // their own, ahead of the rest of the wave.
+    const bool alone = wave.size() == 1;
+    for (int t = 0; t < 2; ++t) {
+      std::vector<int32_t> rowwise;
+      for (int32_t v : wave)
+        if (group_flavor(plan[v].kernel) == kGroupDecoder && kernel_is_f16(plan[v].kernel) == (t == 1)) rowwise.push_back(v);
+      if (rowwise.size() < 2) continue;
+      for (int32_t v : rowwise) {
+        const int64_t tiles = (int64_t)plan[v].gx * plan[v].gy * plan[v].gz;
+        if (members.size() == (size_t)kGroupMaxOps || blocks + tiles > (1 << 24)) { flush(); blocks = 0; }
+        members.push_back(v);
+        blocks += tiles + kGroupAlign;
+      }
+      flush();
+      blocks = 0;
+      wave.erase(std::remove_if(wave.begin(), wave.end(), [&](int32_t v) { return std::count(rowwise.begin(), rowwise.end(), v) != 0; }), wave.end());
+    }
+    if (wave.empty()) continue;
     // A wave that mixes bodies of several flavours is cut between flavours, the heavier
     // members first, wherever the lighter side holds much work: inside a heavier group kernel
     // the lighter members would run at its occupancy (2 or 4 instead of 8 wavefronts per
@@ -271,7 +290,7 @@ int capture_fused(opara_dag *g, opara_exec **out) {
       bool groupable = wave.size() > 1;
       for (int32_t v : wave) {
         const KernelPlan &p = plan[v];
-        const int f = group_flavor(p.kernel);
+        const int f = group_flavor(p.kernel) < 3 ? group_flavor(p.kernel) : -1;
         groupable = groupable && f >= 0 && kernel_is_f16(p.kernel) == kernel_is_f16(plan[wave[0]].kernel) &&
                     (int64_t)p.gx * p.gy * p.gz < (1 << 24);
         if (f >= 0) by_flavor[f].push_back(v);
@@ -302,7 +321,7 @@ int capture_fused(opara_dag *g, opara_exec **out) {
       const KernelPlan &p = plan[v];
       bool light = true;
       const int64_t tiles = (int64_t)p.gx * p.gy * p.gz;
-      const bool fits = group_kernel_ok(p.kernel, &light) && wave.size() > 1 && tiles < (1 << 24);
+      const bool fits = group_kernel_ok(p.kernel, &light) && !alone && tiles < (1 << 24);
       if (!fits) {                                    // on its own, before what follows it in the queue
         flush();
         members.push_back(v);
@@ -1082,7 +1101,8 @@ extern "C" int opara_fused_plan(const opara_exec *e, int32_t *node_of, int32_t *
   if (node_kernel)
     for (size_t i = 0; i < e->fused.size(); ++i) {
       const opara_exec::FusedNode &fn = e->fused[i];
-      node_kernel[i] = fn.is_group ? (fn.flavor == 0 ? OPARA_GROUP_KERNEL_STREAM : fn.flavor == 1 ? OPARA_GROUP_KERNEL_LIGHT : OPARA_GROUP_KERNEL_HEAVY) : fn.plan.kernel;
+      node_kernel[i] = fn.is_group ? (fn.flavor == 0 ? OPARA_GROUP_KERNEL_STREAM : fn.flavor == 1 ? OPARA_GROUP_KERNEL_LIGHT : fn.flavor == 2 ? OPARA_GROUP_KERNEL_HEAVY
+                                                                                                  : OPARA_GROUP_KERNEL_DECODER) : fn.plan.kernel;
     }
   return OPARA_OK;
 }

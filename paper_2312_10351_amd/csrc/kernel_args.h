@@ -88,6 +88,48 @@ struct AttnArgs {
   uint32_t div_gx;              // reciprocal of the grid's width
 };
 
+// Rotary positions; an item is a row and one of `units` chunks of a head's columns.
+struct RotaryArgs {
+  const void *x;
+  void *y;
+  const uint64_t *turns;        // [rotated / 2] turns per position, in units of 2^-64
+  const int32_t *positions;     // [m], or null: first + row
+  int64_t ldx, ldy;             // row strides in elements
+  int32_t heads, width, rotated, first, interleaved;
+  int32_t units, rotated_units; // chunks per head; of these, chunks of the pairs' first halves
+  int32_t heads_each;           // heads per thread (blockIdx.y counts runs of them)
+  uint32_t items, div_units;
+  float amplitude;
+  int32_t reserved;
+};
+
+// Norms around a residual sum (see OPARA_RESIDUAL_NORM).
+struct NormArgs {
+  const void *x, *r, *g, *w;    // block result, residual and gate (null: none), weights (null: ones)
+  const float *b;               // null: zeros
+  void *y, *s;                  // the next block's norm, the sum (either may be null)
+  int32_t rows, cols;
+  int32_t gate_rows;            // rows that share a gate row
+  int32_t rms, after, before;
+  uint32_t div_gate;
+  float eps, alpha, beta;
+};
+
+// Attention (see OPARA_ATTENTION).  blockIdx: x = tile of query rows * splits + split, y = key head, z = sequence.
+struct AttendArgs {
+  const void *q, *k, *v;
+  void *y;
+  const int32_t *lengths;       // [batch] or null
+  uint32_t *counters;           // [batch * kv_heads * tiles], zero between launches (splits > 1)
+  float *partials;              // [batch * kv_heads * tiles * splits][16 * padded width + 32]
+  int64_t q_s[3], k_s[3], v_s[3], y_s[3];   // elements between sequences, rows, heads
+  int32_t m, n, share, width, v_width;      // share: query heads per key head
+  int32_t causal, first;        // causal: 0 no, 1 from `first`, 2 to the sequence's end
+  int32_t tiles, splits;
+  uint32_t div_share, div_splits;
+  float scale;                  // alpha * log2(e): exponentials are powers of two
+};
+
 // X(name, ArgsType).  Order defines kernel ids.
 #define OPARA_KERNEL_LIST(X)            \
   X(igemm_f16_t128x64, IgemmArgs)       \
@@ -156,7 +198,29 @@ struct AttnArgs {
   X(igemm_f32_quad64x64_tail, IgemmArgs) \
   X(igemm_f32_tile64x64_tail, IgemmArgs) \
   X(igemm_f32_t128x64_tail, IgemmArgs) \
-  X(igemm_f32_tile128x128_tail, IgemmArgs)
+  X(igemm_f32_tile128x128_tail, IgemmArgs) \
+  X(rotary_f16, RotaryArgs)             \
+  X(rotary_f32, RotaryArgs)             \
+  X(resnorm_f16_wave, NormArgs)         \
+  X(resnorm_f16_block, NormArgs)        \
+  X(resnorm_f16_wide, NormArgs)         \
+  X(resnorm_f32_wave, NormArgs)         \
+  X(resnorm_f32_block, NormArgs)        \
+  X(resnorm_f32_wide, NormArgs)         \
+  X(gated_f16_any, IgemmArgs)           \
+  X(gated_f32_any, IgemmArgs)           \
+  X(attend_f16_rows64, AttendArgs)      \
+  X(attend_f16_rows128, AttendArgs)     \
+  X(attend_f16_rows256, AttendArgs)     \
+  X(attend_f16_any64, AttendArgs)       \
+  X(attend_f16_any128, AttendArgs)      \
+  X(attend_f16_any256, AttendArgs)      \
+  X(attend_f32_rows64, AttendArgs)      \
+  X(attend_f32_rows128, AttendArgs)     \
+  X(attend_f32_rows256, AttendArgs)     \
+  X(attend_f32_any64, AttendArgs)       \
+  X(attend_f32_any128, AttendArgs)      \
+  X(attend_f32_any256, AttendArgs)
 
 enum KernelId : int32_t {
 #define X(name, T) K_##name,
@@ -173,7 +237,11 @@ union KernelArgs {
   EltArgs elt;
   ConcatArgs concat;
   AttnArgs attn;
+  RotaryArgs rotary;
+  NormArgs norm;
+  AttendArgs attend;
 };
+static_assert(sizeof(KernelArgs) == sizeof(IgemmArgs), "group records hold sixteen of these");
 
 // An element-wise operator computed by the contraction that produces one of its inputs (fused
 // executor): y = f(sum of n_in inputs), all without gaps and of the contraction's size.
@@ -252,6 +320,10 @@ constexpr int kRowCacheChunks = 4;    // 16-byte chunks a thread keeps in regist
 constexpr int kAttnMaxCols = 512;     // attention kernel: one 16-byte chunk of scores per lane of a wavefront
 constexpr int kAttnMaxWidth = 64;     // ... one 128-byte line per row of q, k and v
 constexpr int kGemvMaxM = 4;
+constexpr int kNormWaveChunks = 2, kNormBlockChunks = 8;   // 16-byte chunks a thread of the residual norm keeps
+constexpr int kGatedAnyRows = 64, kGatedAnyCols = 32;      // tile of the gated block's general form
+constexpr int kAttendRows = 16;       // query rows per workgroup
+constexpr int kAttendMaxWidth = 256;
 constexpr int kGapShare = 1;          // global average: log2 of the threads that share a pixel (vector form)
 constexpr int kGapVecMinPixels = 128; // ... taken from this many pixels on
 

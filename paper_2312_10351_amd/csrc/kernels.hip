@@ -1476,6 +1476,10 @@ __device__ __forceinline__ void concat_body(const AR &a, const Blk &b, unsigned 
 }
 
 #include "attention.h"
+#include "rotary.h"
+#include "residual_norm.h"
+#include "gated.h"
+#include "attend.h"
 
 }  // namespace opara
 
@@ -1487,6 +1491,7 @@ constexpr int lds_tile(int bn, int bm, int stages) { return stages * (bn + bm) *
 constexpr int lds_split(int ni, int nj, int s) { return 4 * split_ring_bytes(ni, nj, s); }
 constexpr int lds_direct(int waves) { return waves * 32 * 36 * 4; }
 constexpr int kLdsGap = 4 * 64 * 4, kLdsRow = 16, kLdsNone = 0;
+constexpr int kLdsGatedAny = 2 * 2 * 64 * 80;
 // ... of the bodies that group and chained kernels hold: the most a node of theirs asks for.
 constexpr int kLdsLargestBody = std::max({lds_igemm(64, 64), lds_tile(128, 128, 2), lds_tile(64, 64, 3), lds_tile(128, 64, 2),
                                           lds_split(1, 1, 3), lds_split(2, 2, 2), lds_split(4, 2, 1), lds_split(4, 4, 1), lds_direct(4)});
@@ -1636,6 +1641,29 @@ KDEF2(igemm_f32_quad4s, 256, 3, lds_split(1, 1, 3), IgemmArgs, (igemm_split_body
 KDEFT(igemm_f32_quad4s_tail, 256, 3, lds_split(1, 1, 3), IgemmArgs, (igemm_split_body<float, 1, 1, 3, 0>(a, b, lds, tail)))
 
 KDEF2(attention_f16, 256, 2, kLdsAttention, AttnArgs, (attention_body(a, b, lds)))
+
+// The blocks of a decoder.
+#define DECODER_BODIES(X, T, tn)                                                                              \
+  X(rotary_##tn, RotaryArgs, (rotary_body<T>(a, b, lds)))                                                     \
+  X(resnorm_##tn##_wave, NormArgs, (residual_norm_body<T, 64, kNormWaveChunks>(a, b, lds)))                   \
+  X(resnorm_##tn##_block, NormArgs, (residual_norm_body<T, 256, kNormBlockChunks>(a, b, lds)))                \
+  X(resnorm_##tn##_wide, NormArgs, (residual_norm_wide_body<T>(a, b, lds)))
+#define KDECODER(name, Args, call) KDEF(name, 256, kLdsRow, Args, call)
+DECODER_BODIES(KDECODER, half_t, f16)
+DECODER_BODIES(KDECODER, float, f32)
+#undef KDECODER
+KDEF(gated_f16_any, 256, kLdsGatedAny, IgemmArgs, (gated_any_body<half_t>(a, b, lds)))
+KDEF(gated_f32_any, 256, kLdsGatedAny, IgemmArgs, (gated_any_body<float>(a, b, lds)))
+#define KATTEND(tn, T, dp)                                                                                    \
+  KDEF(attend_##tn##_rows##dp, 256, lds_attend_rows(dp), AttendArgs, (attend_rows_body<T, dp, true>(a, b, lds))) \
+  KDEF(attend_##tn##_any##dp, 256, lds_attend_rows(dp), AttendArgs, (attend_rows_body<T, dp, false>(a, b, lds)))
+KATTEND(f16, half_t, 64)
+KATTEND(f16, half_t, 128)
+KATTEND(f16, half_t, 256)
+KATTEND(f32, float, 64)
+KATTEND(f32, float, 128)
+KATTEND(f32, float, 256)
+#undef KATTEND
 
 // The 256-thread bodies by the vector registers they need (see the group kernels below):
 // X(kernel name, argument record, body call); T / tn: element type, C: access policy.
@@ -2002,7 +2030,14 @@ __device__ __forceinline__ void group_body() {
     CA &a = *(CA *)&ga.args[i];                               \
     call;                                                     \
   } break;
-  if constexpr (F16) {
+  if constexpr (FLAVOR == 3) {
+    typedef typename std::conditional<F16, half_t, float>::type T;
+    if constexpr (F16) {
+      switch (me.kernel) { DECODER_BODIES(GCASE, T, f16) default: break; }
+    } else {
+      switch (me.kernel) { DECODER_BODIES(GCASE, T, f32) default: break; }
+    }
+  } else if constexpr (F16) {
     switch (me.kernel) {
       STREAM_BODIES(GCASE, half_t, 8, f16, 0)
       default:
@@ -2056,6 +2091,8 @@ GROUPK(f16_heavy, 2, true, 2)
 GROUPK(f32_stream, 8, false, 0)
 GROUPK(f32_light, 4, false, 1)
 GROUPK(f32_heavy, 2, false, 2)
+GROUPK(f16_decoder, 2, true, 3)
+GROUPK(f32_decoder, 2, false, 3)
 #undef GROUPK
 
 // ---------------------------------------------------------------------------------
@@ -2323,12 +2360,11 @@ hipError_t add_token_node(hipGraph_t graph, const KernelPlan &p, const TokenArgs
 
 namespace {
 void *group_func(bool f16, int flavor, bool traced) {
-  static void *const f[2][2][3] = {
-      {{(void *)opara_k_group_f32_stream, (void *)opara_k_group_f32_light, (void *)opara_k_group_f32_heavy},
-       {(void *)opara_k_group_f16_stream, (void *)opara_k_group_f16_light, (void *)opara_k_group_f16_heavy}},
-      {{(void *)opara_k_group_f32_stream_traced, (void *)opara_k_group_f32_light_traced, (void *)opara_k_group_f32_heavy_traced},
-       {(void *)opara_k_group_f16_stream_traced, (void *)opara_k_group_f16_light_traced, (void *)opara_k_group_f16_heavy_traced}}};
-  return f[traced ? 1 : 0][f16 ? 1 : 0][flavor < 0 ? 0 : flavor > 2 ? 2 : flavor];
+#define FLAVORS(tn, t) {(void *)opara_k_group_##tn##_stream##t, (void *)opara_k_group_##tn##_light##t, \
+                        (void *)opara_k_group_##tn##_heavy##t, (void *)opara_k_group_##tn##_decoder##t}
+  static void *const f[2][2][kGroupFlavors] = {{FLAVORS(f32, ), FLAVORS(f16, )}, {FLAVORS(f32, _traced), FLAVORS(f16, _traced)}};
+#undef FLAVORS
+  return f[traced ? 1 : 0][f16 ? 1 : 0][flavor < 0 ? 0 : flavor >= kGroupFlavors ? kGroupFlavors - 1 : flavor];
 }
 }  // namespace
 
@@ -2337,6 +2373,7 @@ int group_flavor(int id) {
 #define FCASE(name, Args, call) case K_##name:
     HEAVY_BODIES(FCASE, half_t, f16, 0) HEAVY_BODIES(FCASE, float, f32, 0) FAR_BODIES(FCASE, half_t, f16, 0) FAR_BODIES(FCASE, float, f32, 0) return 2;
     LIGHT_BODIES(FCASE, half_t, f16, 0) LIGHT_BODIES(FCASE, float, f32, 0) return 1;
+    DECODER_BODIES(FCASE, half_t, f16) DECODER_BODIES(FCASE, float, f32) return kGroupDecoder;
 #undef FCASE
     default: return id >= 0 && id < K_attention_f16 ? 0 : -1;     // merged operators run as launches of their own
   }
@@ -2345,14 +2382,14 @@ int group_flavor(int id) {
 bool group_kernel_ok(int id, bool *light) {
   const int f = group_flavor(id);
   *light = f >= 0 && f < 2;
-  return f >= 0;
+  return f >= 0 && f != kGroupDecoder;
 }
 
 // The limit is the kernel's, not the executor's: it is the same for every capture, so that none
 // lowers it under an executor that is still in use.
 hipError_t group_prepare() {
   for (int f16 = 0; f16 < 2; ++f16)
-    for (int flavor = 0; flavor < 3; ++flavor)
+    for (int flavor = 0; flavor < kGroupFlavors; ++flavor)
       for (int traced = 0; traced < 2; ++traced) {
         hipError_t err = hipFuncSetAttribute(group_func(f16, flavor, traced), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsLargestBody);
         if (err != hipSuccess) return err;

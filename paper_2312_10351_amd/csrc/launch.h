@@ -14,9 +14,12 @@ hipError_t add_plan_node(hipGraph_t graph, const KernelPlan &p, const hipGraphNo
 hipError_t add_noop_node(hipGraph_t graph, const hipGraphNode_t *deps, size_t n_deps, hipGraphNode_t *node);
 
 // Group nodes (fused executor): whether a kernel's body can run inside a group kernel at
-// all (256-thread bodies) and inside the light flavour (at most 128 vector registers).
+// all (256-thread bodies; kGroupDecoder apart) and inside the light flavour (at most 128 vector registers).
 bool group_kernel_ok(int kernel_id, bool *light);
-// Flavour of group kernel a body needs: 0 stream (at most 64 vector registers), 1 light (128), 2 heavy; -1 none.
+// Flavour of group kernel a body needs: 0 stream (at most 64 vector registers), 1 light (128), 2 heavy,
+// kGroupDecoder: a decoder's row-wise operators, which group among themselves (the other group kernels, and the
+// chained one, keep their registers); -1 none.
+constexpr int kGroupDecoder = 3, kGroupFlavors = 4;
 int group_flavor(int kernel_id);
 hipError_t add_group_node(hipGraph_t graph, bool f16, int flavor, const GroupArgs &ga, uint32_t n_blocks,
                           uint32_t lds_bytes, const hipGraphNode_t *deps, size_t n_deps, hipGraphNode_t *node);

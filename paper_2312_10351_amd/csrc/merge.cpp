@@ -158,6 +158,9 @@ std::vector<Range> touched(const opara_dag *g, int32_t v) {
       for (int q = 0; q < p.args.concat.n_in; ++q) add(p.args.concat.in[q], (int64_t)p.args.concat.rows * p.args.concat.cols[q]);
       add(p.args.concat.y, (int64_t)p.args.concat.rows * p.args.concat.out_cols);
       break;
+    case OPARA_ROTARY: case OPARA_RESIDUAL_NORM: case OPARA_GATED: case OPARA_ATTENTION:
+      r.push_back({0, UINTPTR_MAX});               // not looked into: may touch anything
+      break;
     default:
       for (int q = 0; q < p.args.elt.n_in; ++q) add(p.args.elt.in[q], p.args.elt.n);
       add(p.args.elt.y, p.args.elt.n);

@@ -21,6 +21,7 @@ struct PersistImage {
 struct opara_dag {
   int32_t n = 0;
   std::vector<opara_op_desc> ops;
+  std::vector<opara_op_more> more;  // one per operator
   std::vector<void *> ext;
   opara_limits lim{};
   // CSR adjacency over operator ids; predecessors in argument order, deduplicated.
@@ -59,7 +60,9 @@ int sync_keep_mask(const opara_dag *g, std::vector<uint8_t> *keep);
 // one the persistent executor runs (two contraction kernels, its own hand-over point between
 // them).  Returns an opara_status.
 enum { kPlanGraph = 0, kPlanPersistent = 1 };
-int plan_op(const opara_op_desc &op, const void *const *in, int kind, KernelPlan *out);
+int plan_op(const opara_op_desc &op, const opara_op_more &more, const void *const *in, int kind, KernelPlan *out);
+// The blocks of a decoder: one plan, of the graph executors.
+int plan_decoder(const opara_op_desc &op, const opara_op_more &more, const void *const *in, KernelPlan *out);
 
 // Operators of consecutive waves that the fused executor runs as one kernel, each
 // the only operator of its wave; the kernel is launched in the place of the first.

@@ -376,7 +376,7 @@ bool tile_choice_open(int kernel_id) {
                      [&](const TileKernel &t) { return t.ids[0] == kernel_id || t.ids[1] == kernel_id; });
 }
 
-int plan_op(const opara_op_desc &op, const void *const *in, int kind, KernelPlan *out) {
+int plan_op(const opara_op_desc &op, const opara_op_more &more, const void *const *in, int kind, KernelPlan *out) {
   std::memset(out, 0, sizeof *out);
   int rc;
   switch (op.op_type) {
@@ -386,6 +386,7 @@ int plan_op(const opara_op_desc &op, const void *const *in, int kind, KernelPlan
     case OPARA_LAYERNORM: case OPARA_SOFTMAX: rc = plan_row(op, in, out); break;
     case OPARA_GELU: case OPARA_RELU: case OPARA_ADD: rc = plan_elt(op, in, out); break;
     case OPARA_CONCAT: rc = plan_concat(op, in, out); break;
+    case OPARA_ROTARY: case OPARA_RESIDUAL_NORM: case OPARA_GATED: case OPARA_ATTENTION: rc = plan_decoder(op, more, in, out); break;
     default: set_error("unknown operator type %d", op.op_type); return OPARA_EINVAL;
   }
   if (rc != OPARA_OK) return rc;

@@ -1,0 +1,273 @@
+// Launch planning of a decoder's blocks: rotary positions, the norms around a residual sum, the gated
+// half of a feed-forward block, attention (host only, no HIP calls).
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include "opara_internal.h"
+
+namespace opara {
+namespace {
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int fail(const char *what, const opara_op_desc &op) {
+  set_error("operator type %d: %s", op.op_type, what);
+  return OPARA_EINVAL;
+}
+int too_large(const char *what, const opara_op_desc &op) {
+  set_error("operator type %d: %s", op.op_type, what);
+  return OPARA_EUNSUPPORTED;
+}
+constexpr int64_t kInt = INT32_MAX;
+
+int plan_rotary(const opara_op_desc &op, const opara_op_more &q, const void *const *in, KernelPlan *out) {
+  const opara_op_params &p = op.params;
+  const bool f16 = op.dtype == OPARA_F16;
+  const int ve = f16 ? 8 : 4;
+  if (op.n_inputs > 2 || !op.weight) return fail("rotary positions take one or two inputs and a table of frequencies", op);
+  if (p.m <= 0 || q.heads <= 0 || q.width <= 0 || q.width > 4096 || q.rotated < 2 || q.rotated > q.width || q.rotated % 2)
+    return fail("bad rotary shape", op);
+  const int64_t cols = (int64_t)q.heads * q.width;
+  if (cols > kInt) return fail("bad rotary shape", op);
+  if ((p.a_row_stride != 0 && p.a_row_stride < cols) || (p.c_row_stride != 0 && p.c_row_stride < cols))
+    return fail("row stride below heads * width", op);
+  RotaryArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.x = in[0]; a.y = op.out; a.turns = (const uint64_t *)op.weight;
+  a.positions = op.n_inputs > 1 ? (const int32_t *)in[1] : nullptr;
+  a.ldx = p.a_row_stride ? p.a_row_stride : cols;
+  a.ldy = p.c_row_stride ? p.c_row_stride : cols;
+  a.heads = q.heads; a.width = q.width; a.rotated = q.rotated; a.first = q.first;
+  a.interleaved = (p.flags & OPARA_FLAG_INTERLEAVED) ? 1 : 0;
+  a.rotated_units = (int32_t)cdiv(q.rotated / 2, ve);
+  a.units = (int32_t)(a.interleaved ? cdiv(q.width, ve) : a.rotated_units + cdiv(q.width - q.rotated, ve));
+  const int64_t items = (int64_t)p.m * a.units;
+  if (items > kInt) return too_large("more rows than one launch holds", op);
+  a.items = (uint32_t)items;
+  a.div_units = div_magic(a.units);
+  a.amplitude = p.alpha;
+  a.heads_each = q.heads;
+  const int64_t blocks = cdiv(items, 256);
+  a.heads_each = (int32_t)std::max<int64_t>(1, std::min<int64_t>(8, blocks * q.heads / 1024));
+  a.heads_each = (int32_t)std::max<int64_t>(a.heads_each, cdiv(q.heads, 65535));
+  out->kernel = f16 ? K_rotary_f16 : K_rotary_f32;
+  out->gx = (uint32_t)blocks; out->gy = (uint32_t)cdiv(q.heads, a.heads_each); out->gz = 1; out->block = 256;
+  out->args.rotary = a;
+  return OPARA_OK;
+}
+
+int plan_norm(const opara_op_desc &op, const opara_op_more &q, const void *const *in, KernelPlan *out) {
+  const opara_op_params &p = op.params;
+  const bool f16 = op.dtype == OPARA_F16;
+  const int ve = f16 ? 8 : 4;
+  if (op.n_inputs > 3) return fail("residual norm takes a block result, a residual and a gate", op);
+  if (p.m <= 0 || p.n <= 0) return fail("bad residual norm shape", op);
+  if (p.batch < 0 || (p.batch > 0 && p.m % p.batch)) return fail("rows must be a multiple of the gate's rows", op);
+  if (op.n_inputs < 3 && p.batch > 0) return fail("gate rows without a gate", op);
+  if (!(p.eps >= 0.f)) return fail("negative eps", op);
+  const bool after = p.flags & OPARA_FLAG_NORM_AFTER, before = p.flags & OPARA_FLAG_NORM_BEFORE;
+  if (q.out2 && !before) return fail("a second result goes with a norm of the sum", op);
+  if ((op.weight || op.bias) && !after && !before) return fail("weights without a norm", op);
+  NormArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.x = in[0];
+  a.r = op.n_inputs > 1 ? in[1] : nullptr;
+  a.g = op.n_inputs > 2 ? in[2] : nullptr;
+  a.w = op.weight; a.b = op.bias;
+  a.y = before ? op.out : nullptr;
+  a.s = before ? q.out2 : op.out;
+  a.rows = p.m; a.cols = p.n;
+  a.gate_rows = p.batch > 0 ? p.m / p.batch : 1;
+  a.div_gate = div_magic(a.gate_rows);
+  a.rms = (p.flags & OPARA_FLAG_RMS) ? 1 : 0;
+  a.after = after; a.before = before;
+  a.eps = p.eps; a.alpha = p.alpha; a.beta = q.beta;
+  static const int ids[2][3] = {{K_resnorm_f32_wave, K_resnorm_f32_block, K_resnorm_f32_wide},
+                                {K_resnorm_f16_wave, K_resnorm_f16_block, K_resnorm_f16_wide}};
+  const int form = p.n <= 64 * ve * kNormWaveChunks ? 0 : p.n <= 256 * ve * kNormBlockChunks ? 1 : 2;
+  out->kernel = ids[f16][form];
+  out->gx = form == 0 ? (uint32_t)cdiv(p.m, 4) : (uint32_t)p.m;
+  out->gy = out->gz = 1; out->block = 256;
+  out->args.norm = a;
+  return OPARA_OK;
+}
+
+int plan_gated(const opara_op_desc &op, const opara_op_more &q, const void *const *in, KernelPlan *out) {
+  const opara_op_params &p = op.params;
+  const bool f16 = op.dtype == OPARA_F16;
+  if (op.n_inputs != 1 || !op.weight) return fail("the gated block takes one input and a weight", op);
+  if (p.m <= 0 || p.n <= 0 || p.k <= 0 || p.n > kInt / 2) return fail("bad shape of a gated block", op);
+  if (q.activation < 0 || q.activation >= OPARA_N_ACTIVATIONS) return fail("unknown activation", op);
+  if ((p.a_row_stride != 0 && p.a_row_stride < p.k) || (p.c_row_stride != 0 && p.c_row_stride < p.n))
+    return fail("row stride below the row", op);
+  IgemmArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.x = in[0]; a.w = op.weight; a.bias = op.bias; a.y = op.out;
+  a.M = p.m; a.N = p.n; a.K = p.k;
+  a.lda = p.a_row_stride ? p.a_row_stride : p.k;
+  a.ldb = p.k;
+  a.ldy = p.c_row_stride ? p.c_row_stride : p.n;
+  a.relu = q.activation;
+  a.alpha = 1.0f;
+  a.HoWo = a.Wo = a.Cin = a.kw = 1;
+  if (p.m > kInt - 64 || p.k > kInt - 64) return too_large("more rows or columns than one launch holds", op);
+  out->kernel = f16 ? K_gated_f16_any : K_gated_f32_any;
+  out->gx = (uint32_t)cdiv(p.m, kGatedAnyRows); out->gy = (uint32_t)cdiv(p.n, kGatedAnyCols); out->gz = 1; out->block = 256;
+  if ((int64_t)out->gx * out->gy > kInt) return too_large("more rows or columns than one launch holds", op);
+  a.div_gx = div_magic(out->gx);
+  out->args.igemm = a;
+  return OPARA_OK;
+}
+
+// ---- attention
+struct AttendShape {
+  int64_t batch, heads, kv_heads, share, v_width, strides[4][3];
+  int dp;                                  // both widths padded
+  int64_t tiles, splits, counter_bytes, scratch;
+};
+
+int attend_shape(const opara_op_desc &op, const opara_op_more &q, AttendShape *s) {
+  const opara_op_params &p = op.params;
+  s->batch = p.batch ? p.batch : 1;
+  s->heads = q.heads;
+  s->kv_heads = q.kv_heads ? q.kv_heads : q.heads;
+  s->v_width = q.v_width ? q.v_width : q.width;
+  if (s->batch < 1 || s->batch > 65535 || p.m <= 0 || p.n <= 0 || s->heads <= 0 || s->kv_heads <= 0 || s->heads % s->kv_heads)
+    return fail("bad attention shape", op);
+  if (q.width < 1 || q.width > kAttendMaxWidth || s->v_width < 1 || s->v_width > kAttendMaxWidth) return fail("head width outside 1..256", op);
+  if ((p.flags & OPARA_FLAG_CAUSAL) && (p.flags & OPARA_FLAG_CAUSAL_END)) return fail("one kind of causal mask", op);
+  s->share = s->heads / s->kv_heads;
+  if (s->kv_heads > 65535 || p.n > (1 << 30) || (int64_t)p.m * s->share > (1 << 30)) return too_large("more rows or heads than one launch holds", op);
+  const int64_t rows[4] = {p.m, p.n, p.n, p.m}, heads[4] = {s->heads, s->kv_heads, s->kv_heads, s->heads},
+                width[4] = {q.width, q.width, s->v_width, s->v_width};
+  for (int i = 0; i < 4; ++i) {
+    const int64_t *given = q.strides[i];
+    if (given[0] < 0 || given[1] < 0 || given[2] < 0) return fail("negative stride", op);
+    const bool packed = !(given[0] | given[1] | given[2]);
+    s->strides[i][2] = packed ? width[i] : given[2];
+    s->strides[i][1] = packed ? heads[i] * width[i] : given[1];
+    s->strides[i][0] = packed ? rows[i] * heads[i] * width[i] : given[0];
+  }
+  // Every result element has a place of its own: sorted by their strides, each axis steps over the ones below.
+  {
+    const int64_t *y = s->strides[3];
+    struct Axis { int64_t stride, count; } axis[3] = {{y[0], s->batch}, {y[1], p.m}, {y[2], s->heads}};
+    std::sort(axis, axis + 3, [](const Axis &a, const Axis &b) { return a.stride < b.stride; });
+    int64_t reach = s->v_width;
+    for (const Axis &x : axis) {
+      if (x.count == 1) continue;
+      if (x.stride < reach) return fail("result rows overlap", op);
+      reach += x.stride * (x.count - 1);
+    }
+  }
+  const int widest = std::max(q.width, (int32_t)s->v_width);
+  s->dp = widest <= 64 ? 64 : widest <= 128 ? 128 : 256;
+  s->tiles = cdiv((int64_t)p.m * s->share, kAttendRows);
+  // Workgroups the chip holds at once: two per CU where the ring is small, else one.
+  const int64_t resident = s->dp == 64 ? 512 : 256, work = s->tiles * s->kv_heads * s->batch;
+  const int64_t key_tile = op.dtype == OPARA_F16 ? 32 : 16;
+  // Half a round or more of the chip runs as it is; a workgroup keeps two tiles for each of its wavefronts.
+  s->splits = work * 2 > resident ? 1 : std::max<int64_t>(1, std::min(resident / work, p.n / (key_tile * 8)));
+  s->counter_bytes = cdiv(4 * work, 256) * 256;
+  s->scratch = s->splits > 1 ? s->counter_bytes + work * s->splits * (kAttendRows * s->dp + 2 * kAttendRows) * 4 : 0;
+  return OPARA_OK;
+}
+
+int plan_attention(const opara_op_desc &op, const opara_op_more &q, const void *const *in, KernelPlan *out) {
+  const opara_op_params &p = op.params;
+  const bool f16 = op.dtype == OPARA_F16;
+  const int ve = f16 ? 8 : 4;
+  AttendShape s;
+  const int rc = attend_shape(op, q, &s);
+  if (rc != OPARA_OK) return rc;
+  if (op.n_inputs < 3 || op.n_inputs > 4) return fail("attention takes queries, keys, values and optionally lengths", op);
+  if ((uintptr_t)q.scratch & 255u) return fail("scratch is not 256-byte aligned", op);
+  AttendArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.q = in[0]; a.k = in[1]; a.v = in[2]; a.y = op.out;
+  a.lengths = op.n_inputs > 3 ? (const int32_t *)in[3] : nullptr;
+  std::memcpy(a.q_s, s.strides[0], sizeof a.q_s);
+  std::memcpy(a.k_s, s.strides[1], sizeof a.k_s);
+  std::memcpy(a.v_s, s.strides[2], sizeof a.v_s);
+  std::memcpy(a.y_s, s.strides[3], sizeof a.y_s);
+  a.m = p.m; a.n = p.n; a.share = (int32_t)s.share; a.width = q.width; a.v_width = (int32_t)s.v_width;
+  a.causal = (p.flags & OPARA_FLAG_CAUSAL) ? 1 : (p.flags & OPARA_FLAG_CAUSAL_END) ? 2 : 0;
+  a.first = q.first;
+  a.scale = p.alpha * 1.44269504088896341f;
+  a.tiles = (int32_t)s.tiles;
+  a.splits = s.splits > 1 && q.scratch && q.scratch_bytes >= (uint64_t)s.scratch ? (int32_t)s.splits : 1;
+  if (a.splits > 1) {
+    a.counters = (uint32_t *)q.scratch;
+    a.partials = (float *)((unsigned char *)q.scratch + s.counter_bytes);
+  }
+  a.div_share = div_magic(s.share);
+  a.div_splits = div_magic(a.splits);
+  // Loads straight into workgroup memory need aligned 16-byte pieces, and 32-bit offsets inside a tile of keys.
+  auto vectors = [&](const void *base, const int64_t *st, int64_t width) {
+    return aligned16(base) && width % ve == 0 && st[0] % ve == 0 && st[1] % ve == 0 && st[2] % ve == 0 &&
+           st[1] < (int64_t)kOperandMaxBytes / (64 * 4);
+  };
+  const bool vec = vectors(a.k, a.k_s, a.width) && vectors(a.v, a.v_s, a.v_width);
+  static const int ids[2][2][3] = {
+      {{K_attend_f32_any64, K_attend_f32_any128, K_attend_f32_any256}, {K_attend_f32_rows64, K_attend_f32_rows128, K_attend_f32_rows256}},
+      {{K_attend_f16_any64, K_attend_f16_any128, K_attend_f16_any256}, {K_attend_f16_rows64, K_attend_f16_rows128, K_attend_f16_rows256}}};
+  out->kernel = ids[f16][vec][s.dp == 64 ? 0 : s.dp == 128 ? 1 : 2];
+  const int64_t gx = s.tiles * a.splits;
+  if (gx * s.kv_heads * s.batch > kInt) return too_large("more rows than one launch holds", op);
+  out->gx = (uint32_t)gx; out->gy = (uint32_t)s.kv_heads; out->gz = (uint32_t)s.batch; out->block = 256;
+  out->args.attend = a;
+  return OPARA_OK;
+}
+
+}  // namespace
+
+int plan_decoder(const opara_op_desc &op, const opara_op_more &more, const void *const *in, KernelPlan *out) {
+  switch (op.op_type) {
+    case OPARA_ROTARY: return plan_rotary(op, more, in, out);
+    case OPARA_RESIDUAL_NORM: return plan_norm(op, more, in, out);
+    case OPARA_GATED: return plan_gated(op, more, in, out);
+    default: return plan_attention(op, more, in, out);
+  }
+}
+
+}  // namespace opara
+
+using namespace opara;
+
+extern "C" int opara_rotary_table(int32_t rotated, double base, double factor, double original_length, double low, double high,
+                                  uint64_t *turns) {
+  if (!turns || rotated < 2 || rotated > 4096 || rotated % 2 || !(base > 0.0) || !std::isfinite(base) || !(factor > 0.0) ||
+      !std::isfinite(factor) || !(original_length >= 0.0) || !std::isfinite(original_length) ||
+      (original_length > 0.0 && !(low < high && std::isfinite(low) && std::isfinite(high)))) {
+    set_error("opara_rotary_table: bad argument");
+    return OPARA_EINVAL;
+  }
+  const long double two_pi = 6.283185307179586476925286766559L, turn = 18446744073709551616.0L;
+  for (int32_t i = 0; i < rotated / 2; ++i) {
+    long double f = powl((long double)base, -2.0L * i / rotated) / two_pi;
+    if (original_length > 0.0) {
+      const long double mix = std::min(1.0L, std::max(0.0L, (original_length * f - low) / ((long double)high - low)));
+      f = f * (mix + (1.0L - mix) / factor);
+    } else {
+      f = f / factor;
+    }
+    f -= floorl(f);                                          // whole turns change nothing
+    const long double v = f * turn + 0.5L;
+    turns[i] = v >= turn ? 0 : (uint64_t)v;
+  }
+  return OPARA_OK;
+}
+
+extern "C" int opara_scratch_bytes(const opara_op_desc *op, const opara_op_more *more, uint64_t *bytes) {
+  if (!op || !bytes) { set_error("opara_scratch_bytes: null pointer"); return OPARA_EINVAL; }
+  *bytes = 0;
+  if (op->op_type < 0 || op->op_type >= OPARA_N_OP_TYPES || (op->dtype != OPARA_F32 && op->dtype != OPARA_F16)) {
+    set_error("opara_scratch_bytes: unknown op_type or dtype");
+    return OPARA_EINVAL;
+  }
+  if (op->op_type != OPARA_ATTENTION) return OPARA_OK;
+  AttendShape s;
+  const int rc = attend_shape(*op, more ? *more : opara_op_more{}, &s);
+  if (rc == OPARA_OK) *bytes = (uint64_t)s.scratch;
+  return rc;
+}

@@ -35,8 +35,10 @@ static uint64_t demand_scalar(const opara_demand &d, const opara_limits &lim) {
 }
 
 static int default_class(int32_t op_type) {
-  return (op_type == OPARA_CONV2D || op_type == OPARA_GEMM || op_type == OPARA_BGEMM)
-             ? OPARA_COMP : OPARA_MEM;
+  switch (op_type) {
+    case OPARA_CONV2D: case OPARA_GEMM: case OPARA_BGEMM: case OPARA_GATED: case OPARA_ATTENTION: return OPARA_COMP;
+    default: return OPARA_MEM;
+  }
 }
 
 }  // namespace opara
@@ -47,6 +49,11 @@ extern "C" const char *opara_last_error(void) { return g_err; }
 
 extern "C" int opara_build_dag(const opara_op_desc *ops, int32_t n_ops, void *const *ext_inputs,
                                int32_t n_ext, const opara_limits *lim, opara_dag **out) {
+  return opara_build_dag_more(ops, nullptr, n_ops, ext_inputs, n_ext, lim, out);
+}
+
+extern "C" int opara_build_dag_more(const opara_op_desc *ops, const opara_op_more *more, int32_t n_ops, void *const *ext_inputs,
+                                    int32_t n_ext, const opara_limits *lim, opara_dag **out) {
   if (!ops || !out || n_ops <= 0 || n_ext < 0 || (n_ext > 0 && !ext_inputs)) {
     set_error("opara_build_dag: null pointer or non-positive operator count");
     return OPARA_EINVAL;
@@ -58,6 +65,8 @@ extern "C" int opara_build_dag(const opara_op_desc *ops, int32_t n_ops, void *co
   try {
     g->n = n_ops;
     g->ops.assign(ops, ops + n_ops);
+    if (more) g->more.assign(more, more + n_ops);
+    else g->more.assign(n_ops, opara_op_more{});
     g->ext.assign(ext_inputs, ext_inputs + n_ext);
     g->lim = lim ? *lim : kMi355x;
     if (!g->lim.threads_per_cu || !g->lim.lds_bytes_per_cu || !g->lim.vgpr_lanes_per_cu) {
@@ -83,6 +92,16 @@ extern "C" int opara_build_dag(const opara_op_desc *ops, int32_t n_ops, void *co
         rc = OPARA_EINVAL; break;
       }
       if (!op.out) { set_error("operator %d: null output pointer", v); rc = OPARA_EINVAL; break; }
+      const opara_op_more &mo = g->more[v];
+      const bool decoder = op.op_type == OPARA_ROTARY || op.op_type == OPARA_RESIDUAL_NORM || op.op_type == OPARA_GATED ||
+                           op.op_type == OPARA_ATTENTION;
+      if (decoder && !more) {
+        set_error("operator %d: type %d needs an opara_op_more record (opara_build_dag_more)", v, op.op_type);
+        rc = OPARA_EINVAL; break;
+      }
+      if (mo.out2 && op.op_type != OPARA_RESIDUAL_NORM) {
+        set_error("operator %d: operators of type %d have one result, out2 must be null", v, op.op_type); rc = OPARA_EINVAL; break;
+      }
       if (op.n_deps < 0 || op.n_deps > OPARA_MAX_INPUTS) {
         set_error("operator %d: n_deps %d outside 0..%d", v, op.n_deps, OPARA_MAX_INPUTS);
         rc = OPARA_EINVAL; break;
@@ -94,6 +113,10 @@ extern "C" int opara_build_dag(const opara_op_desc *ops, int32_t n_ops, void *co
         if (u >= n_ops || (u < 0 && (is_dep || -(int64_t)u - 1 >= n_ext))) {
           set_error("operator %d: %s %d refers to %d, out of range", v, is_dep ? "dependency" : "input",
                     is_dep ? i - op.n_inputs : i, u);
+          rc = OPARA_EINVAL; break;
+        }
+        if (!is_dep && mo.result_of[i] != 0 && (mo.result_of[i] != 1 || u < 0 || !g->more[u].out2)) {
+          set_error("operator %d: input %d asks for result %d, which its producer does not write", v, i, mo.result_of[i]);
           rc = OPARA_EINVAL; break;
         }
         if (u < 0) continue;
@@ -145,11 +168,11 @@ extern "C" int opara_build_dag(const opara_op_desc *ops, int32_t n_ops, void *co
       const void *in[OPARA_MAX_INPUTS];
       for (int i = 0; i < op.n_inputs; ++i) {
         const int32_t u = op.inputs[i];
-        in[i] = u < 0 ? g->ext[-(int64_t)u - 1] : g->ops[u].out;
+        in[i] = u < 0 ? g->ext[-(int64_t)u - 1] : g->more[v].result_of[i] ? g->more[u].out2 : g->ops[u].out;
         if (!in[i]) { set_error("operator %d: input %d resolves to a null pointer", v, i); delete g; return OPARA_EINVAL; }
       }
-      rc = plan_op(op, in, kPlanGraph, &g->plan[v]);
-      if (rc == OPARA_OK) rc = plan_op(op, in, kPlanPersistent, &g->plan_persist[v]);
+      rc = plan_op(op, g->more[v], in, kPlanGraph, &g->plan[v]);
+      if (rc == OPARA_OK) rc = plan_op(op, g->more[v], in, kPlanPersistent, &g->plan_persist[v]);
       if (rc != OPARA_OK) { delete g; return rc; }
       g->plan[v].tag = g->plan_persist[v].tag = v;
       const KernelPlan &p = g->plan[v];

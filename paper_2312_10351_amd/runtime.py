@@ -60,6 +60,8 @@ class Session:
         zero_copy_concat: the operator list goes through opara_elide_concats before the DAG is
         built: concatenations of convolution branches are removed, each branch writes its
         channel slice of the concatenated buffer and the readers depend on the branches.
+        Tensors of the workload that are on the device already (torch tensors) are used in place; they have the
+        library's layouts: [H][W][C] images, [N][K] weights, gate rows before the rows they multiply.
         `self.lib_ops[i]` is the workload id of library operator i, `self.lib_id[v]` the
         library id of workload operator v (absent if removed), `self.elided` the removed
         concatenations.  Outputs are still addressed by workload id."""
@@ -82,24 +84,26 @@ class Session:
                     if u < 0:
                         users.setdefault(-u - 1, []).append(op)
             for slot, a in enumerate(wl.ext_inputs):
-                chans = a.shape[-3] if a.ndim >= 3 else 0
-                if a.ndim >= 3 and chans % ve and all(o.type == "conv2d" for o in users.get(slot, [])):
+                chans = a.shape[-3] if a.ndim >= 3 and isinstance(a, np.ndarray) else 0
+                if chans and a.ndim >= 3 and chans % ve and all(o.type == "conv2d" for o in users.get(slot, [])):
                     self.ext_pad[slot] = (chans + ve - 1) // ve * ve
         self.ext_dev = [self._upload(self._to_physical_input(a, self.ext_pad.get(i))) for i, a in enumerate(wl.ext_inputs)]
         self.out_dev = [None] * len(wl.ops)
+        self.out2_dev = {}                  # second results
         self.w_dev, self.b_dev = {}, {}
-        descs = []
+        descs, more = [], []
         for op in wl.ops:
-            d = B.OpDesc()
+            d, e = B.OpDesc(), B.OpMore()
             d.op_type = B.OP_TYPE_IDS[op.type]
             d.op_class = B.CLASS_DEFAULT if class_override is None else class_override[op.id]
             d.dtype = self.dtype_id
             d.n_inputs = len(op.inputs)
             for i, u in enumerate(op.inputs):
                 d.inputs[i] = u
+                e.result_of[i] = 1 if i in op.second else 0
             if demand_override is not None:
                 d.grid_blocks, d.block_threads, d.lds_bytes, d.vgprs = demand_override[op.id]
-            self._fill_params(op, d.params)
+            self._fill_params(op, d.params, e)
             if op.type == "conv2d" and op.inputs[0] < 0 and (-op.inputs[0] - 1) in self.ext_pad:
                 d.params.c_in = self.ext_pad[-op.inputs[0] - 1]
             if op.id in wl.weights:
@@ -110,15 +114,30 @@ class Session:
                     if cpad:
                         wp = np.concatenate([wp, np.zeros(wp.shape[:3] + (cpad - wp.shape[3],), dtype=w.dtype)], axis=3)
                     wp = np.ascontiguousarray(wp)
-                else:
+                elif isinstance(w, np.ndarray) and op.type != "residual_norm":
                     wp = np.ascontiguousarray(w.T)
+                else:
+                    wp = w
                 self.w_dev[op.id] = self._upload(wp)
-                self.b_dev[op.id] = self._upload(b.astype(np.float32))
+                self.b_dev[op.id] = self._upload(b.astype(np.float32) if isinstance(b, np.ndarray) else b)
                 d.weight = self._ptr(self.w_dev[op.id])
                 d.bias = self._ptr(self.b_dev[op.id])
+            elif op.type == "rotary":
+                q = op.params
+                table = B.opara_rotary_table(q["rotated"], q["base"], q["factor"], q["original"], q["low"], q["high"])
+                self.w_dev[op.id] = self._upload(np.array(table, dtype=np.uint64).view(np.int64))
+                d.weight = self._ptr(self.w_dev[op.id])
             self.out_dev[op.id] = self._alloc(int(np.prod(op.out_shape)) * (wl.batch if _is_image(op) else 1))
             d.out = self._ptr(self.out_dev[op.id])
+            if op.type == "residual_norm" and op.params["before"]:
+                self.out2_dev[op.id] = self._alloc(int(np.prod(op.out_shape)))
+                e.out2 = self._ptr(self.out2_dev[op.id])
+            e.scratch_bytes = B.opara_scratch_bytes(d, e)
+            if e.scratch_bytes:
+                self._keep.append(self._scratch(e.scratch_bytes))
+                e.scratch = self._ptr(self._keep[-1])
             descs.append(d)
+            more.append(e)
         ext_ptrs = [self._ptr(t) for t in self.ext_dev]
         self.elided = []                    # workload ids of the concatenations the library removed
         self.lib_ops = list(range(len(wl.ops)))
@@ -144,7 +163,7 @@ class Session:
                     self.out_dev[v] = self.out_dev[c].view(-1, total)[:, off:off + d.params.c_out]
         self.lib_id = {v: i for i, v in enumerate(self.lib_ops)}
         self.descs = descs
-        self.dag = B.opara_build_dag(descs, ext_ptrs)
+        self.dag = B.opara_build_dag_more(descs, [more[v] for v in self.lib_ops], ext_ptrs)
 
     def _numel(self, op_id):
         op = self.wl.ops[op_id]
@@ -155,6 +174,10 @@ class Session:
         if self.device is None:
             return self._fake_ptr(arr.nbytes)
         import torch
+        if isinstance(arr, torch.Tensor):
+            if arr.device != torch.device(self.device) or not arr.is_contiguous():
+                raise ValueError(f"a device tensor of a workload must be contiguous and on {self.device}")
+            return arr
         return torch.from_numpy(np.ascontiguousarray(arr)).to(self.device)
 
     def _alloc(self, numel):
@@ -163,6 +186,12 @@ class Session:
         import torch
         return torch.zeros(numel, dtype=torch.float32 if self.wl.dtype == "f32" else torch.float16,
                            device=self.device)
+
+    def _scratch(self, nbytes):
+        if self.device is None:
+            return self._fake_ptr(nbytes)
+        import torch
+        return torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
 
     def _elsize(self):
         return 4 if self.wl.dtype == "f32" else 2
@@ -177,14 +206,14 @@ class Session:
 
     @staticmethod
     def _to_physical_input(a, pad_to=None):
-        if a.ndim < 3:
+        if a.ndim < 3 or not isinstance(a, np.ndarray):
             return a
         hwc = np.moveaxis(a, -3, -1)                  # [..., C, H, W] -> [..., H, W, C]
         if pad_to:
             hwc = np.concatenate([hwc, np.zeros(hwc.shape[:-1] + (pad_to - hwc.shape[-1],), dtype=a.dtype)], axis=-1)
         return np.ascontiguousarray(hwc)
 
-    def _fill_params(self, op, p):
+    def _fill_params(self, op, p, e):
         q, t = op.params, op.type
         if t in ("conv2d", "maxpool", "avgpool", "gavgpool"):
             p.c_in, p.h_in, p.w_in = op.in_shapes[0]
@@ -213,6 +242,25 @@ class Session:
                 p.b_batch_stride, p.b_row_stride = d, h * d
                 p.c_batch_stride, p.c_row_stride = d, h * d
                 p.flags |= B.FLAG_B_KMAJOR
+        elif t == "rotary":
+            p.m = op.out_shape[0]
+            p.alpha = q["alpha"]
+            e.heads, e.width, e.rotated, e.first = q["heads"], q["width"], q["rotated"], q["first"]
+            if q["interleaved"]:
+                p.flags |= B.FLAG_INTERLEAVED
+        elif t == "residual_norm":
+            p.m, p.n = op.out_shape
+            p.alpha, e.beta, p.eps, p.batch = q["alpha"], q["beta"], q["eps"], q["gates"]
+            for key, flag in (("after", B.FLAG_NORM_AFTER), ("before", B.FLAG_NORM_BEFORE), ("rms", B.FLAG_RMS)):
+                if q[key]:
+                    p.flags |= flag
+        elif t == "gated":
+            p.m, p.n, p.k, e.activation = q["m"], q["n"], q["k"], B.ACTIVATION_IDS[q["activation"]]
+        elif t == "attention":
+            p.batch, p.m, p.n, p.alpha = q["batch"], q["m"], q["n"], q["alpha"]
+            e.heads, e.kv_heads, e.width, e.v_width, e.first = q["heads"], q["kv_heads"], q["width"], q["v_width"], q["first"]
+            if q["causal"] is not None:
+                p.flags |= {"start": B.FLAG_CAUSAL, "end": B.FLAG_CAUSAL_END}[q["causal"]]
         elif t == "concat":
             if q["axis"] == 0:
                 p.m = op.out_shape[1] * op.out_shape[2] * self.wl.batch
@@ -363,16 +411,30 @@ class Session:
         B.opara_run_eager(self.dag, st.handles[0])
         st.torch_streams[0].synchronize()
 
+    def launch(self, stream=None):
+        """Enqueue every operator in topological order on a torch stream (None: the current one of the
+        session's device): no graph, and nothing waits.  The results are in `result(...)` in that stream's order."""
+        import torch
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device)
+        with torch.cuda.device(self.device):
+            B.opara_run_eager(self.dag, stream.cuda_stream)
+
     def clear_outputs(self):
-        for t in self.out_dev:
+        for t in self.out_dev + list(self.out2_dev.values()):
             t.zero_()
         import torch
         torch.cuda.synchronize()
 
-    def output(self, op_id):
+    def result(self, op_id, second=False):
+        """The buffer of an operator's result (matrices: in the operator's shape) on the device."""
+        t, op = self.out2_dev[op_id] if second else self.out_dev[op_id], self.wl.ops[op_id]
+        return t if _is_image(op) else t.view(op.out_shape)
+
+    def output(self, op_id, second=False):
         """Operator output as a numpy array in the logical layout of the workload."""
         op = self.wl.ops[op_id]
-        a = self.out_dev[op_id].cpu().numpy()
+        a = (self.out2_dev[op_id] if second else self.out_dev[op_id]).cpu().numpy()
         if _is_image(op):
             c, h, w = op.out_shape
             if self.wl.batch > 1:

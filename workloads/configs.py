@@ -16,6 +16,10 @@ CONFIG_NAMES = ("inception_block", "googlenet_like", "inception_v3_like",
                 "bert_base_like", "random_wide_dag", "nasnet_like")
 
 
+class Second(int):
+    """An operator's id that stands for its second result."""
+
+
 class Builder:
     """Tiny DAG builder: appends operators, tracks output shapes."""
 
@@ -23,9 +27,13 @@ class Builder:
         self.name, self.dtype, self.batch = name, dtype, batch
         self.ops = []
         self.ext_shapes = []
+        self.ext_values = {}
 
-    def ext(self, shape):
+    def ext(self, shape, values=None):
+        """An external tensor; with `values` (positions, lengths) int32 of these, not drawn."""
         self.ext_shapes.append(tuple(shape))
+        if values is not None:
+            self.ext_values[len(self.ext_shapes) - 1] = np.asarray(values, dtype=np.int32).reshape(shape)
         return -len(self.ext_shapes)
 
     def shape(self, t):
@@ -33,7 +41,8 @@ class Builder:
 
     def add(self, type_, inputs, in_shapes, out_shape, params=None, name=""):
         op = Op(len(self.ops), type_, list(inputs), [tuple(s) for s in in_shapes],
-                tuple(out_shape), dict(params or {}), name or f"{type_}{len(self.ops)}")
+                tuple(out_shape), dict(params or {}), name or f"{type_}{len(self.ops)}",
+                tuple(i for i, u in enumerate(inputs) if isinstance(u, Second)))
         self.ops.append(op)
         return op.id
 
@@ -79,11 +88,54 @@ class Builder:
     def rowwise(self, kind, xs, r, c, params=None, name=""):
         return self.add(kind, xs, [(r, c)] * len(xs), (r, c), params or {}, name)
 
+    # ---- the blocks of a decoder, logical [rows, heads * width]
+    def rotary(self, x, heads, width, rotated=None, interleaved=False, first=0, positions=None, base=10000.0, factor=1.0,
+               original=0.0, low=1.0, high=4.0, alpha=1.0, name=""):
+        """Rotary positions of every head's first `rotated` columns; row r stands at first + r or at positions[r]."""
+        m = self.shape(x)[0]
+        p = dict(heads=heads, width=width, rotated=rotated or width, interleaved=bool(interleaved), first=first, base=base,
+                 factor=factor, original=original, low=low, high=high, alpha=alpha)
+        extra = [] if positions is None else [positions]
+        return self.add("rotary", [x] + extra, [(m, heads * width)] + [(m,)] * len(extra), (m, heads * width), p, name)
+
+    def residual_norm(self, x, residual=None, gate=None, rms=True, after=False, before=True, alpha=1.0, beta=1.0, eps=1e-5,
+                      weights=True, name=""):
+        """s = alpha * residual + beta * gate * (norm of) x; the result is the norm of s and, as second result
+        (`Second(id)`), s; without `before` it is s."""
+        m, n = self.shape(x)
+        inputs, shapes = [x], [(m, n)]
+        if residual is not None:
+            inputs.append(residual)
+            shapes.append((m, n))
+        if gate is not None:
+            assert residual is not None, "a gate goes with a residual"
+            inputs.append(gate)
+            shapes.append(tuple(self.shape(gate)))
+        p = dict(rms=bool(rms), after=bool(after), before=bool(before), alpha=alpha, beta=beta, eps=eps, gates=shapes[2][0] if gate is not None else 0,
+                 weights=bool(weights) and (after or before))
+        return self.add("residual_norm", inputs, shapes, (m, n), p, name)
+
+    def gated(self, x, m, k, n, activation="silu", name=""):
+        """activation(x . w[:, :n]) * (x . w[:, n:])"""
+        return self.add("gated", [x], [(m, k)], (m, n), dict(m=m, k=k, n=n, activation=activation), name)
+
+    def attention(self, q, k, v, heads, width, kv_heads=None, v_width=None, batch=1, lengths=None, causal=None, first=0, alpha=None, name=""):
+        """Attention of `batch` sequences' query rows to key rows of another number; causal: None, "start" (row i sees
+        i + first + 1 keys) or "end" (the last row sees all of its sequence)."""
+        kv_heads, v_width = kv_heads or heads, v_width or width
+        m, n = self.shape(q)[0] // batch, self.shape(k)[0] // batch
+        p = dict(heads=heads, kv_heads=kv_heads, width=width, v_width=v_width, batch=batch, m=m, n=n, causal=causal, first=first,
+                 alpha=1.0 / float(np.sqrt(width)) if alpha is None else alpha)
+        inputs = [q, k, v] + ([] if lengths is None else [lengths])
+        shapes = [(batch * m, heads * width), (batch * n, kv_heads * width), (batch * n, kv_heads * v_width)] + [(batch,)] * (len(inputs) - 3)
+        return self.add("attention", inputs, shapes, (batch * m, heads * v_width), p, name)
+
     def build(self, seed, random_bias=False, w_std=0.02, he_init=False):
         rng = np.random.Generator(np.random.PCG64(seed))
         npdt = np.float32 if self.dtype == "f32" else np.float16
         lead = lambda s: ((self.batch,) + s) if (self.batch > 1 and len(s) == 3) else s
-        ext = [rng.standard_normal(lead(s), dtype=np.float32).astype(npdt) for s in self.ext_shapes]
+        ext = [self.ext_values[i] if i in self.ext_values else rng.standard_normal(lead(s), dtype=np.float32).astype(npdt)
+               for i, s in enumerate(self.ext_shapes)]
         weights = {}
         for op in self.ops:
             p = op.params
@@ -91,6 +143,13 @@ class Builder:
                 wshape, nb = (p["cout"], p["cin"], p["kh"], p["kw"]), p["cout"]
             elif op.type == "gemm":
                 wshape, nb = (p["k"], p["n"]), p["n"]
+            elif op.type == "gated":
+                wshape, nb = (p["k"], 2 * p["n"]), 2 * p["n"]
+            elif op.type == "residual_norm" and p["weights"]:
+                wshape = (int(p["after"]) + int(p["before"]), op.out_shape[1])
+                w = 1.0 + 0.1 * rng.standard_normal(wshape, dtype=np.float32)
+                weights[op.id] = {"w": w.astype(npdt), "b": (0.1 * rng.standard_normal(wshape, dtype=np.float32)).astype(npdt)}
+                continue
             else:
                 continue
             w = rng.standard_normal(wshape, dtype=np.float32)
@@ -246,6 +305,41 @@ def bert_base_like(seed=BASE_SEED + 3, dtype="f16", layers=12, seq=128, hidden=7
         f2 = b.gemm(g, seq, ffn, hidden, name=f"{t}.ffn2")
         a2 = b.rowwise("add", [f2, n1], seq, hidden, name=f"{t}.add2")
         x = b.rowwise("layernorm", [a2], seq, hidden, {"eps": 1e-5}, f"{t}.ln2")
+    return b.build(seed)
+
+
+def decoder_like(seed=BASE_SEED + 6, dtype="f16", layers=2, seq=77, states=128, hidden=768, heads=12, kv_heads=4, ffn=2048, past=0):
+    """Decoder of an encoder-decoder model over `seq` rows: causal self attention with rotary positions and
+    shared key and value heads, attention to `states` rows of an encoder, gated feed-forward, and
+    the sum of every block fused with the next block's norm.  The projections of the encoder's
+    states depend on nothing in the decoder: every layer's can run beside anything.  past: position of the first row."""
+    b = Builder("decoder_like", dtype)
+    d = hidden // heads
+    x, enc = b.ext((seq, hidden)), b.ext((states, hidden))
+    n = b.residual_norm(x, name="norm0")
+    s = x
+    for l in range(layers):
+        t = f"L{l}"
+        q = b.gemm(n, seq, hidden, heads * d, name=f"{t}.q")
+        k = b.gemm(n, seq, hidden, kv_heads * d, name=f"{t}.k")
+        v = b.gemm(n, seq, hidden, kv_heads * d, name=f"{t}.v")
+        rq = b.rotary(q, heads, d, first=past, name=f"{t}.rotary_q")
+        rk = b.rotary(k, kv_heads, d, first=past, name=f"{t}.rotary_k")
+        a = b.attention(rq, rk, v, heads, d, kv_heads, causal="start", name=f"{t}.self")
+        o = b.gemm(a, seq, heads * d, hidden, name=f"{t}.self_out")
+        n = b.residual_norm(o, s, name=f"{t}.norm1")
+        s = Second(n)
+        q = b.gemm(n, seq, hidden, heads * d, name=f"{t}.cross_q")
+        k = b.gemm(enc, states, hidden, kv_heads * d, name=f"{t}.cross_k")
+        v = b.gemm(enc, states, hidden, kv_heads * d, name=f"{t}.cross_v")
+        a = b.attention(q, k, v, heads, d, kv_heads, name=f"{t}.cross")
+        o = b.gemm(a, seq, heads * d, hidden, name=f"{t}.cross_out")
+        n = b.residual_norm(o, s, name=f"{t}.norm2")
+        s = Second(n)
+        g = b.gated(n, seq, hidden, ffn, name=f"{t}.gated")
+        o = b.gemm(g, seq, ffn, hidden, name=f"{t}.down")
+        n = b.residual_norm(o, s, name=f"{t}.norm3")
+        s = Second(n)
     return b.build(seed)
 
 

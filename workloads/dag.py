@@ -14,9 +14,9 @@ from typing import Dict, List, Tuple
 import numpy as np
 
 OP_TYPES = ("conv2d", "gemm", "bgemm", "maxpool", "avgpool", "gavgpool", "concat",
-            "layernorm", "softmax", "gelu", "relu", "add")
+            "layernorm", "softmax", "gelu", "relu", "add", "rotary", "residual_norm", "gated", "attention")
 # operator-table classes (paper Sec. 3.3: compute-intensive vs memory-intensive)
-COMPUTE_TYPES = ("conv2d", "gemm", "bgemm")
+COMPUTE_TYPES = ("conv2d", "gemm", "bgemm", "gated", "attention")
 
 
 @dataclass
@@ -28,6 +28,7 @@ class Op:
     out_shape: Tuple[int, ...]
     params: Dict = field(default_factory=dict)
     name: str = ""
+    second: Tuple[int, ...] = ()      # places among `inputs` that take their producer's second result
 
 
 @dataclass
@@ -35,7 +36,7 @@ class Workload:
     name: str
     dtype: str                        # "f32" | "f16"
     ops: List[Op]
-    ext_inputs: List[np.ndarray]      # already rounded to dtype
+    ext_inputs: List[np.ndarray]      # already rounded to dtype; positions and lengths are int32
     weights: Dict[int, Dict[str, np.ndarray]]  # op id -> {"w": ..., "b": ...}, rounded to dtype
     seed: int = 0
     batch: int = 1                    # images per pass; image tensors are then [batch, C, H, W]
