@@ -208,7 +208,19 @@ struct AttendArgs {
   X(resnorm_f32_block, NormArgs)        \
   X(resnorm_f32_wide, NormArgs)         \
   X(gated_f16_any, IgemmArgs)           \
+  X(gated_f16_row, IgemmArgs)          \
+  X(gated_f16_split16, IgemmArgs)       \
+  X(gated_f16_split32, IgemmArgs)       \
+  X(gated_f16_split64, IgemmArgs)       \
+  X(gated_f16_tile64, IgemmArgs)        \
+  X(gated_f16_tile128, IgemmArgs)       \
   X(gated_f32_any, IgemmArgs)           \
+  X(gated_f32_row, IgemmArgs)          \
+  X(gated_f32_split16, IgemmArgs)       \
+  X(gated_f32_split32, IgemmArgs)       \
+  X(gated_f32_split64, IgemmArgs)       \
+  X(gated_f32_tile128, IgemmArgs)       \
+  X(gated_f16_tile256, IgemmArgs)       \
   X(attend_f16_rows64, AttendArgs)      \
   X(attend_f16_rows128, AttendArgs)     \
   X(attend_f16_rows256, AttendArgs)     \
@@ -321,6 +333,7 @@ constexpr int kAttnMaxCols = 512;     // attention kernel: one 16-byte chunk of 
 constexpr int kAttnMaxWidth = 64;     // ... one 128-byte line per row of q, k and v
 constexpr int kGemvMaxM = 4;
 constexpr int kNormWaveChunks = 2, kNormBlockChunks = 8;   // 16-byte chunks a thread of the residual norm keeps
+constexpr int kGatedRowMaxCols = 1024;                    // one row: up to here a wavefront per column
 constexpr int kGatedAnyRows = 64, kGatedAnyCols = 32;      // tile of the gated block's general form
 constexpr int kAttendRows = 16;       // query rows per workgroup
 constexpr int kAttendMaxWidth = 256;

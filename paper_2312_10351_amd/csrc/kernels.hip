@@ -1654,6 +1654,17 @@ DECODER_BODIES(KDECODER, float, f32)
 #undef KDECODER
 KDEF(gated_f16_any, 256, kLdsGatedAny, IgemmArgs, (gated_any_body<half_t>(a, b, lds)))
 KDEF(gated_f32_any, 256, kLdsGatedAny, IgemmArgs, (gated_any_body<float>(a, b, lds)))
+KDEF2(gated_f16_tile256, 512, 2, lds_tile(256, 256, 2), IgemmArgs, (gated_wide_body<256, 256, 4, 2>(a, b, lds)))
+#define KGATED(tn, T)                                                                                         \
+  KDEF(gated_##tn##_row, 256, kLdsNone, IgemmArgs, (gated_row_body<T>(a, b, lds)))                             \
+  KDEF2(gated_##tn##_split16, 256, 2, lds_split(2, 1, 3), IgemmArgs, (gated_split_body<T, 2, 1, 3>(a, b, lds))) \
+  KDEF2(gated_##tn##_split32, 256, 2, lds_split(4, 2, 1), IgemmArgs, (gated_split_body<T, 4, 2, 1>(a, b, lds))) \
+  KDEF2(gated_##tn##_split64, 256, 2, lds_split(4, 4, 1), IgemmArgs, (gated_split_body<T, 4, 4, 1>(a, b, lds))) \
+  KDEF2(gated_##tn##_tile128, 256, 2, lds_tile(128, 128, 2), IgemmArgs, (gated_tile_body<T, 128, 128, 2, 2, 2>(a, b, lds)))
+KDEF2(gated_f16_tile64, 256, 2, lds_tile(128, 64, 2), IgemmArgs, (gated_tile_body<half_t, 128, 64, 2, 2, 2>(a, b, lds)))
+KGATED(f16, half_t)
+KGATED(f32, float)
+#undef KGATED
 #define KATTEND(tn, T, dp)                                                                                    \
   KDEF(attend_##tn##_rows##dp, 256, lds_attend_rows(dp), AttendArgs, (attend_rows_body<T, dp, true>(a, b, lds))) \
   KDEF(attend_##tn##_any##dp, 256, lds_attend_rows(dp), AttendArgs, (attend_rows_body<T, dp, false>(a, b, lds)))

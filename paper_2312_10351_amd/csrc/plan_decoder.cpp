@@ -92,6 +92,29 @@ int plan_norm(const opara_op_desc &op, const opara_op_more &q, const void *const
   return OPARA_OK;
 }
 
+// The forms of the gated block that are fed through workgroup memory, and what one workgroup costs in
+// microseconds, in fp32 and in fp16: a 128-byte step of K with a compute unit to itself (`alone`) and in a full
+// launch (`busy`), and everything outside the K walk (`fixed`).  Fitted to 115 products of each type (1..2048 rows,
+// 256..4096 -> 512..12288, weights in no cache) within 12 %; the form it picks is 2 % slower than the best in the mean.
+struct GatedCost { double alone, busy, fixed; };
+struct GatedForm { int ids[2], rows, cols, threads; GatedCost cost[2]; };            // f32, f16
+const GatedForm kGatedForms[] = {
+    {{K_gated_f32_split16, K_gated_f16_split16}, 16, 16, 256, {{0.103, 0.091, 0.9}, {0.06, 0.066, 0.5}}},
+    {{K_gated_f32_split32, K_gated_f16_split32}, 32, 32, 256, {{0.28, 0.29, 1.2}, {0.14, 0.14, 0.5}}},
+    {{K_gated_f32_split64, K_gated_f16_split64}, 64, 32, 256, {{0.51, 0.52, 2.1}, {0.165, 0.21, 1.4}}},
+    {{-1, K_gated_f16_tile64}, 64, 64, 256, {{0.0, 0.0, 0.0}, {0.56, 0.39, 0.45}}},
+    {{K_gated_f32_tile128, K_gated_f16_tile128}, 128, 64, 256, {{2.03, 1.88, 5.0}, {0.66, 0.56, 2.0}}},
+    {{-1, K_gated_f16_tile256}, 256, 128, 512, {{0.0, 0.0, 0.0}, {1.25, 1.83, 7.0}}},
+};
+double gated_cost(const GatedForm &f, double m, double n, double k, bool f16) {
+  const double es = f16 ? 2.0 : 4.0, steps = std::ceil(k * es / 128.0), tiles = std::ceil(m / f.rows) * std::ceil(n / f.cols);
+  const GatedCost &c = f.cost[f16];
+  double work = tiles * (steps * c.busy + c.fixed) / 256.0;
+  if (tiles > 256.0 && tiles < 1024.0) work *= std::ceil(tiles / 256.0) * 256.0 / tiles;     // whole rounds over the CUs
+  const double bytes = (2.0 * n * k + m * k + m * n) * es / 5.8e6;                           // 5.8 TB/s
+  return std::max({steps * c.alone + c.fixed, work, bytes});
+}
+
 int plan_gated(const opara_op_desc &op, const opara_op_more &q, const void *const *in, KernelPlan *out) {
   const opara_op_params &p = op.params;
   const bool f16 = op.dtype == OPARA_F16;
@@ -111,8 +134,31 @@ int plan_gated(const opara_op_desc &op, const opara_op_more &q, const void *cons
   a.alpha = 1.0f;
   a.HoWo = a.Wo = a.Cin = a.kw = 1;
   if (p.m > kInt - 64 || p.k > kInt - 64) return too_large("more rows or columns than one launch holds", op);
-  out->kernel = f16 ? K_gated_f16_any : K_gated_f32_any;
-  out->gx = (uint32_t)cdiv(p.m, kGatedAnyRows); out->gy = (uint32_t)cdiv(p.n, kGatedAnyCols); out->gz = 1; out->block = 256;
+  auto set = [&](int kernel, int rows, int cols, int threads) {
+    out->kernel = kernel;
+    out->gx = (uint32_t)cdiv(p.m, rows); out->gy = (uint32_t)cdiv(p.n, cols); out->gz = 1; out->block = threads;
+  };
+  const int64_t es = f16 ? 2 : 4, x_bytes = es * ((int64_t)(p.m - 1) * a.lda + p.k), w_bytes = es * 2 * (int64_t)p.n * p.k;
+  // Loads straight into workgroup memory need aligned 16-byte pieces and 32-bit offsets.
+  const bool vec = p.k % (16 / es) == 0 && a.lda % (16 / es) == 0 && aligned16(a.x) && aligned16(a.w) && x_bytes < kOperandMaxBytes &&
+                   w_bytes < kOperandMaxBytes && p.k * es < 1 << 29;
+  a.x_bytes = vec ? (uint32_t)x_bytes : 0;
+  a.w_bytes = vec ? (uint32_t)w_bytes : 0;
+  if (p.m == 1 && (!vec || p.n <= kGatedRowMaxCols)) {
+    set(f16 ? K_gated_f16_row : K_gated_f32_row, 1, 4, 256);
+    std::swap(out->gx, out->gy);
+  } else if (!vec) {
+    set(f16 ? K_gated_f16_any : K_gated_f32_any, kGatedAnyRows, kGatedAnyCols, 256);
+  } else {
+    const GatedForm *best = nullptr;
+    double least = 0.0;
+    for (const GatedForm &f : kGatedForms) {
+      if (f.ids[f16] < 0) continue;
+      const double cost = gated_cost(f, p.m, p.n, p.k, f16);
+      if (!best || cost < least) { best = &f; least = cost; }
+    }
+    set(best->ids[f16], best->rows, best->cols, best->threads);
+  }
   if ((int64_t)out->gx * out->gy > kInt) return too_large("more rows or columns than one launch holds", op);
   a.div_gx = div_magic(out->gx);
   out->args.igemm = a;

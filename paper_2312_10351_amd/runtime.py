@@ -67,6 +67,7 @@ class Session:
         concatenations.  Outputs are still addressed by workload id."""
         self.wl = wl
         self.device = device
+        self._index = None
         self.dag = None
         self.execs = []
         self._workspaces = []
@@ -415,10 +416,14 @@ class Session:
         """Enqueue every operator in topological order on a torch stream (None: the current one of the
         session's device): no graph, and nothing waits.  The results are in `result(...)` in that stream's order."""
         import torch
-        if stream is None:
-            stream = torch.cuda.current_stream(self.device)
-        with torch.cuda.device(self.device):
-            B.opara_run_eager(self.dag, stream.cuda_stream)
+        if self._index is None:
+            self._index = torch.device(self.device).index or 0
+        handle = (torch.cuda.current_stream(self._index) if stream is None else stream).cuda_stream
+        if torch.cuda.current_device() == self._index:     # switching devices costs half as much as a launch
+            B.opara_run_eager(self.dag, handle)
+        else:
+            with torch.cuda.device(self._index):
+                B.opara_run_eager(self.dag, handle)
 
     def clear_outputs(self):
         for t in self.out_dev + list(self.out2_dev.values()):

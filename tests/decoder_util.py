@@ -17,6 +17,12 @@ TINY = {"f16": 2.0 ** -25, "f32": 2.0 ** -149}
 TORCH = {"f16": torch.float16, "f32": torch.float32}
 
 
+# rows, K, columns of gated blocks that take every form the planner has
+GATED = [(1, 8, 1), (1, 64, 33), (2, 768, 2048), (3, 1027, 100), (4, 4096, 512), (5, 256, 96), (16, 512, 130), (17, 40, 31), (33, 320, 640),
+         (64, 64, 64), (77, 768, 2048), (128, 1024, 768), (130, 200, 72), (257, 512, 520), (300, 33, 257), (512, 2048, 1024),
+         (300, 1024, 2100), (520, 512, 4100), (1000, 640, 4000), (2040, 1032, 4090), (256, 264, 4092)]
+
+
 def normal(gen, shape, dtype, std=1.0, mean=0.0):
     return (torch.randn(shape, generator=gen, dtype=torch.float64) * std + mean).to(TORCH[dtype])
 

@@ -6,7 +6,7 @@ from fractions import Fraction
 import numpy as np
 import pytest
 
-from decoder_util import build, describe
+from decoder_util import GATED as GATED_SIZES, build, describe
 from oracle import executor, ops as O
 from paper_2312_10351_amd import binding as B
 from paper_2312_10351_amd.runtime import Session
@@ -189,6 +189,13 @@ def test_scratch_is_asked_for_where_keys_are_shared_out():
     for more in (few[1], None):
         with pytest.raises(B.OparaError):
             B.opara_scratch_bytes(few[0], more)
+
+
+def test_gated_sizes_of_the_gpu_tests_reach_every_form():
+    for dtype in ("f16", "f32"):
+        all_of_them = {B.opara_kernel_info(i)[0] for i in range(B.opara_kernel_count())}
+        taken = {build(describe(B.GATED, dtype, 1, m=m, n=n, k=k, weight=0x2000))[0] for m, k, n in GATED_SIZES}
+        assert taken == {name for name in all_of_them if name.startswith(f"gated_{dtype}_")}
 
 
 # ---- in a DAG ------------------------------------------------------------------------------

@@ -136,19 +136,16 @@ def test_residual_norm_rows_of_zeros():
 
 # ---- the gated block ------------------------------------------------------------------------
 
-GATED = [(1, 8, 1), (1, 64, 33), (2, 768, 2048), (3, 1027, 100), (4, 4096, 512), (5, 256, 96), (16, 512, 130), (17, 40, 31), (33, 320, 640),
-         (64, 64, 64), (77, 768, 2048), (128, 1024, 768), (130, 200, 72), (257, 512, 520), (300, 33, 257), (512, 2048, 1024)]
-
 
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
-@pytest.mark.parametrize("i", range(len(GATED)))
+@pytest.mark.parametrize("i", range(len(D.GATED)))
 def test_gated(dtype, i):
-    m, k, n = GATED[i]
+    m, k, n = D.GATED[i]
     act = list(B.ACTIVATION_IDS)[i % 5]
     g = gen(i)
     x, w, b = D.normal(g, (m, k), dtype), D.normal(g, (2 * n, k), dtype, 1.0 / np.sqrt(k)), D.normal(g, (2 * n,), "f32", 0.1)
     s = D.bind(lambda bl, e: bl.gated(e[0], m, k, n, act), [x], {0: {"w": w, "b": b}}, dtype)
-    D.within(run(s).result(0), *D.gated(x, w, b, act, dtype), dtype, act)
+    D.within(run(s).result(0), *D.gated(*(t.to(DEV) for t in (x, w, b)), act, dtype), dtype, act)
     s.close()
 
 
