@@ -253,8 +253,8 @@ int opara_rotary_table(int32_t rotated, double base, double factor, double origi
  * few query rows shares the keys out between workgroups and joins their results; for that it
  * needs this much device memory, which must hold zeros when the operator first runs and is left so that it
  * can run again.  It belongs to this operator alone; executors of one DAG share it like they share its
- * result buffers, so their replays must not overlap.  Without scratch, or with less than this, one
- * workgroup walks all keys of its query rows.  Looks at op_type, dtype, params and more's shape (more may be NULL
+ * result buffers, so their replays must not overlap.  With less than this fewer
+ * workgroups share the keys, without scratch one walks all keys of its query rows.  Looks at op_type, dtype, params and more's shape (more may be NULL
  * where the operator needs none).  No HIP call.  Errors: as opara_build_dag.
  */
 int opara_scratch_bytes(const opara_op_desc *op, const opara_op_more *more, uint64_t *bytes);

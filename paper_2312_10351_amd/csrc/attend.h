@@ -15,9 +15,8 @@
 // workgroups: each leaves (maximum, sum, result) in scratch memory and the last to arrive joins them in
 // a fixed order, so the result does not depend on who that is.
 
-constexpr int attend_stages(int dp) { return dp <= 128 ? 2 : 1; }
-constexpr int attend_ring_bytes(int dp) { return attend_stages(dp) * 2 * 64 * dp; }      // of one wavefront
-constexpr int lds_attend_rows(int dp) { return 4 * attend_ring_bytes(dp) + 16; }
+constexpr int attend_ring_bytes(int dp) { return 2 * 64 * dp; }      // of one wavefront: a tile of keys, one of values
+constexpr int lds_attend_rows(int dp) { return 4 * attend_ring_bytes(dp); }
 
 // What one tile of sixteen query rows sees: keys [0, end), row r its first limit(r).
 template <typename AR> struct AttendSight {
@@ -35,6 +34,139 @@ template <typename AR> struct AttendSight {
   }
 };
 
+// Four result columns of one query row; `scale`: one over the sum of its probabilities.
+template <typename T, typename AR>
+__device__ __forceinline__ void attend_store(const AR &a, int g, int z, int r, int col, floatx4 v, float scale) {
+  typedef typename Run4<T>::type R;
+  const int i = (int)fast_div((uint32_t)r, (uint32_t)a.share, a.div_share);
+  T *y = (T *)a.y + z * a.y_s[0] + i * a.y_s[1] + (g * a.share + r - i * a.share) * a.y_s[2] + col;
+  if (col + 3 < a.v_width) {
+    *(R *)y = R{(T)(v[0] * scale), (T)(v[1] * scale), (T)(v[2] * scale), (T)(v[3] * scale)};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (col + e < a.v_width) y[e] = (T)(v[e] * scale);
+  }
+}
+// One over a sum of probabilities; a row that has seen nothing gives zeros, NaN stays.
+__device__ __forceinline__ float attend_inverse(float sum) { return sum > 0.f ? 1.0f / sum : sum == 0.f ? 0.f : sum; }
+
+// The workgroups that share a tile's keys meet.  Each has left a record of R maxima, R sums and R x DP results in
+// `slots` with agent-scope stores, which pass the caches that XCDs do not share; it is counted once its stores have
+// completed, and whoever counts last invalidates its caches and joins the records in their order.
+// As in the persistent executor this rests on gfx950's behaviour (a store that vmcnt has retired has
+// reached the memory side all XCDs share), not on a release fence, which would write back a whole L2 per
+// workgroup.  place(q): row and column of the q-th run of four results.  lds: R * splits floats, then 16 bytes per thread.
+template <typename T, int DP, int R, int NT, typename AR, typename F>
+__device__ __forceinline__ void attend_join(const AR &a, int64_t tile_id, const float *slots, int g, int z, int r0, int runs,
+                                            unsigned char *lds, F place) {
+  constexpr int REC = R * DP + 2 * R;
+  const int t = threadIdx.x, S = a.splits, rows = min(R, a.m * a.share - r0);
+  asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+  __syncthreads();
+  int *last = (int *)lds;
+  if (t == 0) {
+    uint32_t *count = a.counters + tile_id;
+    const bool end = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)S - 1u;
+    if (end) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // for the next launch
+    *last = end;
+  }
+  __syncthreads();
+  if (!*last) return;
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+  __syncthreads();                                           // `last` lies where the factors go
+  // ---- what every record counts for in a row: LR lanes share the row's records, eight loads in flight
+  constexpr int LR = NT / R;
+  static_assert(LR >= 1 && LR <= 64 && (LR & (LR - 1)) == 0, "lanes per row");
+  float *factor = (float *)lds;                              // [S][R]
+  {
+    const int row = t / LR, part = t % LR;
+    const float *stat = slots + R * DP + min(row, rows - 1);
+    auto each = [&](auto f) {
+      for (int s0 = part; s0 < S; s0 += 8 * LR) {
+        float m[8], e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float *at = stat + (int64_t)min(s0 + i * LR, S - 1) * REC;
+          m[i] = at[0];
+          e[i] = at[R];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (s0 + i * LR < S) f(s0 + i * LR, m[i], e[i]);
+      }
+    };
+    float most = -INFINITY, total = 0.f;
+    each([&](int, float m, float) { most = fmaxf(most, m); });
+#pragma unroll
+    for (int off = LR / 2; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, 64));
+    each([&](int s, float m, float e) {
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - most);
+      factor[s * R + row] = f;
+      total += f * e;
+    });
+#pragma unroll
+    for (int off = LR / 2; off > 0; off >>= 1) total += __shfl_xor(total, off, 64);
+    const float inverse = attend_inverse(total);
+    for (int s = part; s < S; s += LR) factor[s * R + row] *= inverse;
+  }
+  __syncthreads();
+  // ---- the sums.  Few runs of four results: `parts` threads share one; many: a thread takes eight at a time, so
+  // that as many loads are in flight.
+  if (runs <= NT) {
+    const int parts = runs * 8 <= NT ? 8 : runs * 4 <= NT ? 4 : runs * 2 <= NT ? 2 : 1, q = t % (NT / parts), part = t / (NT / parts);
+    floatx4 *shared = (floatx4 *)(lds + (((size_t)R * S * 4 + 15) & ~(size_t)15));
+    int row, col;
+    place(min(q, runs - 1), row, col);
+    const bool live = q < runs && row < rows && col < a.v_width;
+    floatx4 v = {0.f, 0.f, 0.f, 0.f};
+    if (live) {
+      const float *from = slots + (int64_t)q * 4;
+      int s = part;
+      for (; s + 7 * parts < S; s += 8 * parts) {
+        floatx4 x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = *(const floatx4 *)(from + (int64_t)(s + i * parts) * REC);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v += x[i] * factor[(s + i * parts) * R + row];
+      }
+      for (; s < S; s += parts) v += *(const floatx4 *)(from + (int64_t)s * REC) * factor[s * R + row];
+    }
+    shared[t] = v;
+    __syncthreads();
+    if (live && part == 0) {
+      for (int i = 1; i < parts; ++i) v += shared[i * (NT / parts) + t];
+      attend_store<T>(a, g, z, r0 + row, col, v, 1.0f);
+    }
+    return;
+  }
+  for (int q0 = t; q0 < runs; q0 += 8 * NT) {
+    int row[8];
+    floatx4 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      int c;
+      place(min(q0 + i * NT, runs - 1), row[i], c);
+      row[i] = min(row[i], rows - 1);                        // rows behind the last are computed and not stored
+      v[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    for (int s = 0; s < S; ++s) {
+      const float *from = slots + (int64_t)s * REC;
+      floatx4 x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = *(const floatx4 *)(from + (int64_t)min(q0 + i * NT, runs - 1) * 4);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += x[i] * factor[s * R + row[i]];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      int at, c;
+      place(min(q0 + i * NT, runs - 1), at, c);
+      if (q0 + i * NT < runs && at < rows && c < a.v_width) attend_store<T>(a, g, z, r0 + at, c, v[i], 1.0f);
+    }
+  }
+}
+
 template <typename T, int DP, bool VEC, typename AR>
 __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsigned char *lds) {
   typedef typename Vec16<T>::type V;
@@ -43,9 +175,9 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
   constexpr int KT = 4 * VE;                                // keys per tile: 32 halves or 16 floats deep
   constexpr int CH = DP * ES / 16;                          // 16-byte chunks per key or value row
   constexpr int L = KT * CH / 64;                           // loads of a wavefront per tile of keys, or of values
-  constexpr int S = attend_stages(DP), TILE = KT * DP * ES, RING = attend_ring_bytes(DP);
+  constexpr int TILE = KT * DP * ES, RING = attend_ring_bytes(DP);
   constexpr int NS = DP / (4 * VE), NQ = KT / 16, NO = DP / 16, PITCH = DP + 4;
-  static_assert(RING == 2 * S * TILE && 16 * PITCH * 4 + 128 <= RING, "ring of a wavefront");
+  static_assert(RING == 2 * TILE && 16 * PITCH * 4 + 128 <= RING, "ring of a wavefront");
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int grp = lane >> 4, r16 = lane & 15;
   const int tile = (int)fast_div((uint32_t)b.x, (uint32_t)a.splits, a.div_splits), split = b.x - tile * a.splits;
@@ -55,8 +187,9 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
   const AttendSight<AR> sight(a, z, (int)fast_div((uint32_t)min(rows - 1, r0 + 15), (uint32_t)a.share, a.div_share));
   const int mine = r < rows ? sight.limit(qi) : 0;          // this lane's query row sees keys [0, mine)
   const int tiles = (sight.end + KT - 1) / KT;
-  const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
-  const int bound = min(sight.end, t1 * KT);                // keys of this workgroup end here
+  // Tiles go round the wavefronts of all workgroups that share them: what is read at a time lies together
+  // (65536 keys of 8 heads beside each other, 32 splits: 53.2 us; in runs of tiles 61.1).
+  const int first = split * 4 + wave, step = 4 * a.splits;
 
   V qf[NS];                                                 // query row r16, elements (s * 4 + grp) * VE ..
   {
@@ -76,7 +209,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
     }
   }
   const T *kbase = (const T *)a.k + z * a.k_s[0] + g * a.k_s[2], *vbase = (const T *)a.v + z * a.v_s[0] + g * a.v_s[2];
-  unsigned char *ring = lds + wave * RING;                  // S tiles of keys, then S tiles of values
+  unsigned char *ring = lds + wave * RING;                  // a tile of keys, a tile of values
   // A row's chunk c lies in slot c ^ (row & 7): fragment reads of adjacent rows then differ in their banks.
   const int lrow = lane / CH, lslot = lane % CH;            // row and slot this lane fills (row + l * 64 / CH)
   constexpr int RL = 64 / CH;                               // rows per load
@@ -88,7 +221,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
 #pragma unroll
       for (int l = 0; l < L; ++l) {
         const int row = l * RL + lrow, chunk = lslot ^ (row & 7);
-        const bool in = kt * KT + row < bound && chunk * VE < width;
+        const bool in = kt * KT + row < sight.end && chunk * VE < width;
         lds_load16(buf, in ? ((uint32_t)row * (uint32_t)pitch + (uint32_t)chunk * VE) * ES : kOperandMaxBytes, 0,
                    lds_address(to) + l * 1024);
       }
@@ -97,7 +230,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
       for (int l = 0; l < L; ++l) {
         const int row = l * RL + lrow, chunk = lslot ^ (row & 7), key = kt * KT + row, d = chunk * VE;
         V v = {};
-        if (key < bound) {
+        if (key < sight.end) {
           const T *src = base + (int64_t)key * pitch + d;
           if (d + VE <= width) v = *(const VU *)src;
           else
@@ -109,30 +242,28 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
       }
     }
   };
-  auto stage_k = [&](int kt, int slot) { stage(kbase, a.k_s[1], a.width, kt, ring + slot * TILE); };
-  auto stage_v = [&](int kt, int slot) { stage(vbase, a.v_s[1], a.v_width, kt, ring + (S + slot) * TILE); };
+  auto stage_k = [&](int kt) { stage(kbase, a.k_s[1], a.width, kt, ring); };
+  auto stage_v = [&](int kt) { stage(vbase, a.v_s[1], a.v_width, kt, ring + TILE); };
 
   floatx4 o[NO];
 #pragma unroll
   for (int j = 0; j < NO; ++j) o[j] = floatx4{0.f, 0.f, 0.f, 0.f};
   float top = -INFINITY, sum = 0.f;
-  int kt = t0 + wave;
-  // Tiles past the range load nothing (zeros), so that the number of loads in flight never varies.
+  int kt = first;
+  // Keys are refilled as soon as they have been read, behind them the values: while one product runs
+  // the other's operand is on its way.  (Two slots each hold half the workgroups per CU and measured the same.)  Tiles past
+  // the last load nothing (zeros), so that the number of loads in flight never varies.
   if constexpr (VEC) {
-    if (kt < t1) {
-#pragma unroll
-      for (int s = 0; s < S; ++s) { stage_k(kt + s * 4, s); stage_v(kt + s * 4, s); }
-    }
+    if (kt < tiles) { stage_k(kt); stage_v(kt); }
   }
-  int slot = 0;
 #pragma nounroll
-  for (; kt < t1; kt += 4) {
-    if constexpr (VEC) wait_loads<(2 * S - 1) * L>();
-    else stage_k(kt, slot);
+  for (; kt < tiles; kt += step) {
+    if constexpr (VEC) wait_loads<L>();
+    else stage_k(kt);
     // ---- scores of KT keys
     float p[NQ][4];
     {
-      const unsigned char *K = ring + slot * TILE;
+      const unsigned char *K = ring;
 #pragma unroll
       for (int i = 0; i < NQ; ++i) {
         floatx4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -147,7 +278,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
     }
     if constexpr (VEC) {
       asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the slot has been read: it may be refilled
-      stage_k(kt + S * 4, slot);
+      stage_k(kt + step);
     }
     // ---- running maximum and sum
     float most = top;
@@ -173,9 +304,9 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[j][e] *= shrink;
     // ---- O^T += V^T P^T; key e of a lane's step: 16 * (e / 4) + 4 * grp + e % 4
-    if constexpr (VEC) wait_loads<(2 * S - 1) * L>();
-    else stage_v(kt, slot);
-    const unsigned char *W = ring + (S + slot) * TILE;
+    if constexpr (VEC) wait_loads<L>();
+    else stage_v(kt);
+    const unsigned char *W = ring + TILE;
     V pf;
 #pragma unroll
     for (int e = 0; e < VE; ++e) pf[e] = (T)p[e / 4][e % 4];
@@ -204,9 +335,8 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
     }
     if constexpr (VEC) {
       asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-      stage_v(kt + S * 4, slot);
+      stage_v(kt + step);
     }
-    slot = slot == S - 1 ? 0 : slot + 1;
   }
 
   // ---- the four wavefronts meet
@@ -230,88 +360,214 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
     share[w] = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - all);
     total += share[w] * wave0[w * WF + 16 * PITCH + 16 + pr];
   }
-  const int row = r0 + pr, yi = (int)fast_div((uint32_t)row, (uint32_t)a.share, a.div_share);
-  T *y = (T *)a.y + z * a.y_s[0] + yi * a.y_s[1] + (g * a.share + row - yi * a.share) * a.y_s[2];
+  const int row = r0 + pr;
   auto joined = [&](int col) {
     floatx4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const floatx4 x = *(const floatx4 *)(wave0 + w * WF + pr * PITCH + col);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += share[w] * x[e];
-    }
+    for (int w = 0; w < 4; ++w) v += *(const floatx4 *)(wave0 + w * WF + pr * PITCH + col) * share[w];
     return v;
   };
-  auto store = [&](int col, floatx4 v, float total) {
-    typedef typename Run4<T>::type R;
-    const float inv = total > 0.f ? 1.0f / total : total == 0.f ? 0.f : total;      // nothing seen: zeros; NaN stays
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] *= inv;
-    if (col + 3 < a.v_width) {
-      *(R *)(y + col) = R{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (col + e < a.v_width) y[col + e] = (T)v[e];
-    }
-  };
   if (a.splits == 1) {
+    const float inverse = attend_inverse(total);
     if (row < rows)
 #pragma unroll
       for (int c = 0; c < DP; c += 64)
-        if (c + pc < a.v_width) store(c + pc, joined(c + pc), total);
+        if (c + pc < a.v_width) attend_store<T>(a, g, z, row, c + pc, joined(c + pc), inverse);
     return;
   }
-
-  // ---- the workgroups of a tile meet.  Partial results go past the caches that XCDs do not share
-  // (agent-scope stores); a workgroup is counted once its stores have completed, and whoever counts last
-  // invalidates its caches and reads them all.  As in the persistent executor this rests on
-  // gfx950's behaviour (a store that vmcnt has retired has reached the memory side all XCDs
-  // share), not on a release fence, which would write back a whole L2 per workgroup.
   const int64_t tile_id = ((int64_t)z * b.gy + g) * a.tiles + tile;
-  float *slot0 = a.partials + tile_id * a.splits * (16 * DP + 32), *mineslot = slot0 + (int64_t)split * (16 * DP + 32);
+  float *slots = a.partials + tile_id * a.splits * (16 * DP + 32), *mineslot = slots + (int64_t)split * (16 * DP + 32);
   if (row < rows) {
 #pragma unroll
-    for (int c = 0; c < DP; c += 64) {
-      const floatx4 v = joined(c + pc);
-      stg<true, floatx4>(mineslot + pr * DP + c + pc, v);
-    }
+    for (int c = 0; c < DP; c += 64) stg<true, floatx4>(mineslot + pr * DP + c + pc, joined(c + pc));
     if ((t & 15) == 0) {
       stg<true, float>(mineslot + 16 * DP + pr, all);
       stg<true, float>(mineslot + 16 * DP + 16 + pr, total);
     }
   }
-  asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-  __syncthreads();
-  int *last = (int *)(lds + 4 * RING);
-  if (t == 0) {
-    uint32_t *count = a.counters + tile_id;
-    const bool end = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)a.splits - 1u;
-    if (end) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // for the next launch
-    *last = end;
+  attend_join<T, DP, 16, 256>(a, tile_id, slots, g, z, r0, min(16, rows - r0) * (DP / 4), lds, [](int q, int &row, int &col) {
+    row = q / (DP / 4);
+    col = q % (DP / 4) * 4;
+  });
+}
+
+
+// wide kernels, fp16: 32 NW query rows per workgroup, 32 per wavefront, the keys in tiles of 64 that all
+// wavefronts share, two of them and their values in workgroup memory.  32 x 32 matrix instructions: a lane holds a
+// query row and half the keys of a tile, so that a row's statistics take one exchange.
+// What bounds it: per tile and wavefront 64 x 32 x 2 widths of matrix work, about as long in vector instructions
+// (exponentials take a quarter of the rate) and in fragment reads; two wavefronts per SIMD overlap the three.
+// The result is scaled down only when a row's maximum has grown by more than 2^kAttendSlack: until
+// then probabilities may exceed one, by at most that, which their rounding, relative to each, does not see.
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+constexpr float kAttendSlack = 8.f;
+constexpr int lds_attend_wide(int dp) { return 4 * 64 * dp * 2; }
+
+template <int DP, int NW, typename AR>
+__device__ __forceinline__ void attend_wide_body(const AR &a, const Blk &b, unsigned char *lds) {
+  typedef half_t T;
+  typedef half8 V;
+  typedef V VU __attribute__((aligned(2)));
+  constexpr int KT = 64, CH = DP / 8, TILE = KT * DP * 2;     // keys per tile, 16-byte chunks per row, bytes
+  constexpr int L = TILE / 1024 / NW, RL = 64 / CH;           // loads of a wavefront per tile, rows per load
+  constexpr int NS = DP / 16, NO = DP / 32;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int hi = lane >> 5, r32 = lane & 31, r16 = lane & 15;
+  // Every XCD takes a contiguous range of (sequence, key head, tile): its L2 then holds one head's keys.  The tiles
+  // of a head in descending order: under a causal mask the later rows have more to do.
+  int tile, split, g, z;
+  {
+    const uint32_t total = (uint32_t)(b.gx * b.gy * a.batch), lin = (uint32_t)b.lin + (uint32_t)(b.gx * b.gy) * (uint32_t)b.z;
+    const uint32_t xcd = lin % 8u, r = total % 8u, at = xcd * (total / 8u) + (xcd < r ? xcd : r) + lin / 8u;
+    const uint32_t head = at / (uint32_t)b.gx;
+    const int x = b.gx - 1 - (int)(at - head * (uint32_t)b.gx);
+    z = (int)(head / (uint32_t)b.gy);
+    g = (int)(head - (uint32_t)z * (uint32_t)b.gy);
+    tile = (int)fast_div((uint32_t)x, (uint32_t)a.splits, a.div_splits);
+    split = x - tile * a.splits;
   }
-  __syncthreads();
-  if (!*last) return;
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-  if (row >= rows) return;
-  float most = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) most = fmaxf(most, slot0[(int64_t)s * (16 * DP + 32) + 16 * DP + pr]);
-  floatx4 v[DP / 64];
+  const int r0 = tile * (32 * NW), rows = a.m * a.share;
+  const int r = r0 + wave * 32 + r32, qi = (int)fast_div((uint32_t)r, (uint32_t)a.share, a.div_share), head = g * a.share + r - qi * a.share;
+  const AttendSight<AR> sight(a, z, (int)fast_div((uint32_t)min(rows - 1, r0 + 32 * NW - 1), (uint32_t)a.share, a.div_share));
+  const int mine = r < rows ? sight.limit(qi) : 0;
+  const int last = min(rows - 1, r0 + wave * 32 + 31);        // of this wavefront; it sees keys below `reach`
+  const int reach = r0 + wave * 32 < rows ? sight.limit((int)fast_div((uint32_t)last, (uint32_t)a.share, a.div_share)) : 0;
+  const int all = sight.limit((int)fast_div((uint32_t)r0, (uint32_t)a.share, a.div_share));   // every row of the tile sees these
+  const int tiles = (sight.end + KT - 1) / KT, full = all / KT;
+
+  V qf[NS];
+  {
+    const T *q = (const T *)a.q + z * a.q_s[0] + qi * a.q_s[1] + head * a.q_s[2];
 #pragma unroll
-  for (int c = 0; c < DP / 64; ++c) v[c] = floatx4{0.f, 0.f, 0.f, 0.f};
-  float whole = 0.f;
-  for (int s = 0; s < a.splits; ++s) {
-    const float *from = slot0 + (int64_t)s * (16 * DP + 32);
-    const float ms = from[16 * DP + pr], f = ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - most);
-    whole += f * from[16 * DP + 16 + pr];
+    for (int s = 0; s < NS; ++s) {
+      const int d = s * 16 + hi * 8;
+      V v = {};
+      if (r < rows) {
+        if (d + 8 <= a.width) v = *(const VU *)(q + d);
+        else
 #pragma unroll
-    for (int c = 0; c < DP / 64; ++c) {
-      const floatx4 x = *(const floatx4 *)(from + pr * DP + c * 64 + pc);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[c][e] += f * x[e];
+          for (int e = 0; e < 8; ++e)
+            if (d + e < a.width) v[e] = q[d + e];
+      }
+      qf[s] = v;
     }
   }
+  const T *kbase = (const T *)a.k + z * a.k_s[0] + g * a.k_s[2], *vbase = (const T *)a.v + z * a.v_s[0] + g * a.v_s[2];
+  const int lrow = lane / CH, lslot = lane % CH;
+  auto stage = [&](const T *base, int64_t pitch, int width, int kt, unsigned char *to) {
+    const i32x4 buf = buffer_of(base + (int64_t)kt * KT * pitch, kOperandMaxBytes);
 #pragma unroll
-  for (int c = 0; c < DP / 64; ++c)
-    if (c * 64 + pc < a.v_width) store(c * 64 + pc, v[c], whole);
+    for (int l = 0; l < L; ++l) {
+      const int row = (wave * L + l) * RL + lrow, chunk = lslot ^ (row & 7);
+      const bool in = kt * KT + row < sight.end && chunk * 8 < width;
+      lds_load16(buf, in ? ((uint32_t)row * (uint32_t)pitch + (uint32_t)chunk * 8) * 2u : kOperandMaxBytes, 0,
+                 lds_address(to) + (wave * L + l) * 1024);
+    }
+  };
+  auto issue = [&](int kt, int slot) {
+    stage(kbase, a.k_s[1], a.width, kt, lds + slot * TILE);
+    stage(vbase, a.v_s[1], a.v_width, kt, lds + (2 + slot) * TILE);
+  };
+  floatx16 o[NO] = {};
+  float top = -INFINITY, sum = 0.f;
+  if (split < tiles) issue(split, 0);
+  int slot = 0;
+  auto step = [&](int kt, auto masked_tag) {
+    constexpr bool MASKED = decltype(masked_tag)::value;
+    wait_loads_and_meet<0>();
+    const unsigned char *K = lds + slot * TILE, *W = lds + (2 + slot) * TILE;
+    slot ^= 1;
+    if (kt + a.splits < tiles) issue(kt + a.splits, slot);
+    if (MASKED && kt * KT >= reach) return;
+    floatx16 s[2] = {};
+#pragma unroll
+    for (int d = 0; d < NS; ++d)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const V kf = *(const V *)(K + (i * 32 + r32) * (DP * 2) + (((d * 2 + hi) ^ (r32 & 7)) * 16));
+        s[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[d], s[i], 0, 0, 0);
+      }
+    float most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        if constexpr (MASKED) s[i][e] = kt * KT + i * 32 + (e >> 2) * 8 + hi * 4 + (e & 3) < mine ? s[i][e] * a.scale : -INFINITY;
+        most = fmaxf(most, s[i][e]);
+      }
+    if constexpr (!MASKED) most *= a.scale;                   // a positive factor
+    most = fmaxf(most, __shfl_xor(most, 32, 64));
+    if (__any(most > top + kAttendSlack)) {
+      const float now = fmaxf(most, top);
+      const float from = now == -INFINITY ? 0.f : now;
+      const float shrink = __builtin_amdgcn_exp2f(top - from);
+      top = now;
+      sum *= shrink;
+#pragma unroll
+      for (int j = 0; j < NO; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[j][e] *= shrink;
+    }
+    const float from = top == -INFINITY ? 0.f : top;
+    V p[4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float x = __builtin_amdgcn_exp2f(MASKED ? s[i][e] - from : __builtin_fmaf(s[i][e], a.scale, -from));
+        sum += x;
+        p[i * 2 + e / 8][e % 8] = (T)x;
+      }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int j = 0; j < NO; ++j) {
+        half4 v[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int row = q * 16 + h * 8 + hi * 4 + (r16 >> 2);
+          const int chunk = j * 4 + ((lane >> 4) & 1) * 2 + ((r16 >> 1) & 1);
+          v[h] = lds_read_transposed(W + row * (DP * 2) + ((chunk ^ (row & 7)) * 16) + (r16 & 1) * 8);
+        }
+        o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7), p[q], o[j], 0, 0, 0);
+      }
+  };
+  int kt = split;
+#pragma nounroll
+  for (; kt < full; kt += a.splits) step(kt, std::integral_constant<bool, false>{});
+#pragma nounroll
+  for (; kt < tiles; kt += a.splits) step(kt, std::integral_constant<bool, true>{});
+  sum += __shfl_xor(sum, 32, 64);
+  if (a.splits == 1) {
+    const float inverse = attend_inverse(sum);
+    if (r < rows)
+#pragma unroll
+      for (int j = 0; j < NO; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int col = j * 32 + q * 8 + hi * 4;
+          if (col < a.v_width)
+            attend_store<T>(a, g, z, r, col, floatx4{o[j][q * 4], o[j][q * 4 + 1], o[j][q * 4 + 2], o[j][q * 4 + 3]}, inverse);
+        }
+    return;
+  }
+  // A record keeps the results as the lanes hold them, so that they are written and read in whole lines.
+  constexpr int R = 32 * NW, REC = R * DP + 2 * R;
+  const int64_t tile_id = ((int64_t)z * b.gy + g) * a.tiles + tile;
+  float *slots = a.partials + tile_id * a.splits * REC, *mineslot = slots + (int64_t)split * REC;
+#pragma unroll
+  for (int j = 0; j < NO; ++j)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      stg<true, floatx4>(mineslot + ((wave * (DP / 8) + j * 4 + q) * 64 + lane) * 4,
+                         floatx4{o[j][q * 4], o[j][q * 4 + 1], o[j][q * 4 + 2], o[j][q * 4 + 3]});
+  if (hi == 0) {
+    stg<true, float>(mineslot + R * DP + wave * 32 + r32, top);
+    stg<true, float>(mineslot + R * DP + R + wave * 32 + r32, sum);
+  }
+  attend_join<T, DP, R, 64 * NW>(a, tile_id, slots, g, z, r0, R * DP / 4, lds, [](int q, int &row, int &col) {
+    const int lane = q & 63, run = (q >> 6) % (DP / 8);
+    row = (q >> 6) / (DP / 8) * 32 + (lane & 31);
+    col = run * 8 + (lane >> 5) * 4;
+  });
 }

@@ -124,7 +124,7 @@ struct AttendArgs {
   float *partials;              // [batch * kv_heads * tiles * splits][16 * padded width + 32]
   int64_t q_s[3], k_s[3], v_s[3], y_s[3];   // elements between sequences, rows, heads
   int32_t m, n, share, width, v_width;      // share: query heads per key head
-  int32_t causal, first;        // causal: 0 no, 1 from `first`, 2 to the sequence's end
+  int32_t batch, causal, first; // causal: 0 no, 1 from `first`, 2 to the sequence's end
   int32_t tiles, splits;
   uint32_t div_share, div_splits;
   float scale;                  // alpha * log2(e): exponentials are powers of two
@@ -224,6 +224,9 @@ struct AttendArgs {
   X(attend_f16_rows64, AttendArgs)      \
   X(attend_f16_rows128, AttendArgs)     \
   X(attend_f16_rows256, AttendArgs)     \
+  X(attend_f16_wide64, AttendArgs)      \
+  X(attend_f16_wide128, AttendArgs)     \
+  X(attend_f16_huge128, AttendArgs)     \
   X(attend_f16_any64, AttendArgs)       \
   X(attend_f16_any128, AttendArgs)      \
   X(attend_f16_any256, AttendArgs)      \
@@ -337,6 +340,10 @@ constexpr int kGatedRowMaxCols = 1024;                    // one row: up to here
 constexpr int kGatedAnyRows = 64, kGatedAnyCols = 32;      // tile of the gated block's general form
 constexpr int kAttendRows = 16;       // query rows per workgroup
 constexpr int kAttendMaxWidth = 256;
+// Workgroups that share the keys of a tile: the join keeps a factor for each of its rows in workgroup memory
+// (rows kernels: at most 256 x 16 of 32 KB, wide ones 32 x 128 or 32 x 256).
+constexpr int64_t kAttendMaxSplits = 256, kAttendMaxWideSplits = 32;
+constexpr int64_t kAttendMaxScratch = (int64_t)1 << 30;
 constexpr int kGapShare = 1;          // global average: log2 of the threads that share a pixel (vector form)
 constexpr int kGapVecMinPixels = 128; // ... taken from this many pixels on
 

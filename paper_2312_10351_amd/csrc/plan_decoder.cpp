@@ -168,8 +168,8 @@ int plan_gated(const opara_op_desc &op, const opara_op_more &q, const void *cons
 // ---- attention
 struct AttendShape {
   int64_t batch, heads, kv_heads, share, v_width, strides[4][3];
-  int dp;                                  // both widths padded
-  int64_t tiles, splits, counter_bytes, scratch;
+  int dp;                                  // both widths padded: 64, 128 or 256
+  double keys;                             // what a query row sees of n in the mean, as far as the host knows
 };
 
 int attend_shape(const opara_op_desc &op, const opara_op_more &q, AttendShape *s) {
@@ -208,21 +208,64 @@ int attend_shape(const opara_op_desc &op, const opara_op_more &q, AttendShape *s
   }
   const int widest = std::max(q.width, (int32_t)s->v_width);
   s->dp = widest <= 64 ? 64 : widest <= 128 ? 128 : 256;
-  s->tiles = cdiv((int64_t)p.m * s->share, kAttendRows);
-  // Workgroups the chip holds at once: two per CU where the ring is small, else one.
-  const int64_t resident = s->dp == 64 ? 512 : 256, work = s->tiles * s->kv_heads * s->batch;
-  const int64_t key_tile = op.dtype == OPARA_F16 ? 32 : 16;
-  // Half a round or more of the chip runs as it is; a workgroup keeps two tiles for each of its wavefronts.
-  s->splits = work * 2 > resident ? 1 : std::max<int64_t>(1, std::min(resident / work, p.n / (key_tile * 8)));
-  s->counter_bytes = cdiv(4 * work, 256) * 256;
-  s->scratch = s->splits > 1 ? s->counter_bytes + work * s->splits * (kAttendRows * s->dp + 2 * kAttendRows) * 4 : 0;
+  const double first = p.flags & OPARA_FLAG_CAUSAL ? (double)q.first : (double)p.n - p.m;
+  s->keys = p.n;
+  if (p.flags & (OPARA_FLAG_CAUSAL | OPARA_FLAG_CAUSAL_END)) s->keys = std::min<double>(p.n, std::max(1.0, first + 0.5 * p.m));
   return OPARA_OK;
+}
+
+// What the forms of attention cost: nanoseconds per key for a workgroup with a compute unit to itself (`alone`) and in
+// a full launch (`busy`), microseconds outside the keys (`fixed`), of a join of several workgroups
+// (`join`) and of every workgroup that is joined (`each`); records pass through memory at 2.5 TB/s.  Fitted to
+// 700 launches per type (1..2048 rows of 1..32 key heads, 128..65536 keys, 1..256 splits); the form and split it
+// picks are 2 % slower than the best in the mean.
+struct AttendForm { int kernel, any, rows, threads, key_tile; double alone, busy, fixed, join, each; };   // any: for unaligned keys, -1 none
+const AttendForm kAttendF16[3][3] = {
+    {{K_attend_f16_rows64, K_attend_f16_any64, 16, 256, 128, 7.3, 6.3, 3.1, 5.5, 0.10},
+     {K_attend_f16_wide64, -1, 128, 256, 64, 16.9, 11.7, 3.4, 2.4, 0.63},
+     {-1, -1, 0, 0, 0, 0, 0, 0, 0, 0}},
+    {{K_attend_f16_rows128, K_attend_f16_any128, 16, 256, 128, 8.3, 11.5, 4.2, 5.0, 0.25},
+     {K_attend_f16_wide128, -1, 128, 256, 64, 26.9, 21.1, 4.3, 3.5, 0.90},
+     {K_attend_f16_huge128, -1, 256, 512, 64, 32.5, 40.0, 5.6, 3.7, 1.08}},
+    {{K_attend_f16_rows256, K_attend_f16_any256, 16, 256, 128, 16.0, 22.0, 6.0, 5.0, 0.27},
+     {-1, -1, 0, 0, 0, 0, 0, 0, 0, 0},
+     {-1, -1, 0, 0, 0, 0, 0, 0, 0, 0}}};
+const AttendForm kAttendF32[3] = {{K_attend_f32_rows64, K_attend_f32_any64, 16, 256, 64, 18.4, 17.9, 3.1, 5.8, 0.085},
+                                  {K_attend_f32_rows128, K_attend_f32_any128, 16, 256, 64, 28.9, 34.7, 4.2, 5.7, 0.21},
+                                  {K_attend_f32_rows256, K_attend_f32_any256, 16, 256, 64, 54.1, 80.0, 6.6, 5.0, 0.27}};
+
+struct AttendPick { const AttendForm *form; int64_t tiles, splits, counter_bytes, scratch; };
+
+// vec: keys and values can be loaded straight into workgroup memory; room: scratch memory there is.
+AttendPick attend_pick(const opara_op_desc &op, const AttendShape &s, bool vec, uint64_t room) {
+  const bool f16 = op.dtype == OPARA_F16;
+  const int size = s.dp == 64 ? 0 : s.dp == 128 ? 1 : 2;
+  const AttendForm *forms = f16 ? kAttendF16[size] : &kAttendF32[size];
+  AttendPick best{};
+  double least = 0.0;
+  for (int i = 0; i < (f16 ? 3 : 1); ++i) {
+    const AttendForm &f = forms[i];
+    if (f.kernel < 0 || (!vec && f.any < 0) || (f.rows > kAttendRows && !(op.params.alpha > 0.f))) continue;
+    const int64_t tiles = cdiv((int64_t)op.params.m * s.share, f.rows), work = tiles * s.kv_heads * s.batch;
+    for (int64_t n = 1; n <= kAttendMaxSplits; n = n < 4 ? n + 1 : n + n / 2) {
+      if (n > 1 && n * f.key_tile > s.keys) break;           // two tiles for every wavefront
+      if (n > (f.rows == kAttendRows ? kAttendMaxSplits : kAttendMaxWideSplits)) break;
+      AttendPick p{&f, tiles, n, cdiv(4 * work, 256) * 256, 0};
+      const int64_t records = work * n * (f.rows * s.dp + 2 * f.rows) * 4;
+      if (n > 1) p.scratch = p.counter_bytes + records;
+      if ((uint64_t)p.scratch > room || p.scratch > kAttendMaxScratch) break;
+      const double keys = std::ceil(s.keys / (f.key_tile * n)) * f.key_tile;
+      double cost = f.fixed + std::max(keys * f.alone, work * n * keys / 256.0 * f.busy) * 1e-3;
+      if (n > 1) cost += f.join + f.each * n + records / 2.5e6;
+      if (!best.form || cost < least) { best = p; least = cost; }
+    }
+  }
+  return best;
 }
 
 int plan_attention(const opara_op_desc &op, const opara_op_more &q, const void *const *in, KernelPlan *out) {
   const opara_op_params &p = op.params;
-  const bool f16 = op.dtype == OPARA_F16;
-  const int ve = f16 ? 8 : 4;
+  const int ve = op.dtype == OPARA_F16 ? 8 : 4;
   AttendShape s;
   const int rc = attend_shape(op, q, &s);
   if (rc != OPARA_OK) return rc;
@@ -236,31 +279,30 @@ int plan_attention(const opara_op_desc &op, const opara_op_more &q, const void *
   std::memcpy(a.k_s, s.strides[1], sizeof a.k_s);
   std::memcpy(a.v_s, s.strides[2], sizeof a.v_s);
   std::memcpy(a.y_s, s.strides[3], sizeof a.y_s);
-  a.m = p.m; a.n = p.n; a.share = (int32_t)s.share; a.width = q.width; a.v_width = (int32_t)s.v_width;
-  a.causal = (p.flags & OPARA_FLAG_CAUSAL) ? 1 : (p.flags & OPARA_FLAG_CAUSAL_END) ? 2 : 0;
-  a.first = q.first;
-  a.scale = p.alpha * 1.44269504088896341f;
-  a.tiles = (int32_t)s.tiles;
-  a.splits = s.splits > 1 && q.scratch && q.scratch_bytes >= (uint64_t)s.scratch ? (int32_t)s.splits : 1;
-  if (a.splits > 1) {
-    a.counters = (uint32_t *)q.scratch;
-    a.partials = (float *)((unsigned char *)q.scratch + s.counter_bytes);
-  }
-  a.div_share = div_magic(s.share);
-  a.div_splits = div_magic(a.splits);
   // Loads straight into workgroup memory need aligned 16-byte pieces, and 32-bit offsets inside a tile of keys.
   auto vectors = [&](const void *base, const int64_t *st, int64_t width) {
     return aligned16(base) && width % ve == 0 && st[0] % ve == 0 && st[1] % ve == 0 && st[2] % ve == 0 &&
            st[1] < (int64_t)kOperandMaxBytes / (64 * 4);
   };
-  const bool vec = vectors(a.k, a.k_s, a.width) && vectors(a.v, a.v_s, a.v_width);
-  static const int ids[2][2][3] = {
-      {{K_attend_f32_any64, K_attend_f32_any128, K_attend_f32_any256}, {K_attend_f32_rows64, K_attend_f32_rows128, K_attend_f32_rows256}},
-      {{K_attend_f16_any64, K_attend_f16_any128, K_attend_f16_any256}, {K_attend_f16_rows64, K_attend_f16_rows128, K_attend_f16_rows256}}};
-  out->kernel = ids[f16][vec][s.dp == 64 ? 0 : s.dp == 128 ? 1 : 2];
-  const int64_t gx = s.tiles * a.splits;
+  const bool vec = vectors(a.k, a.k_s, q.width) && vectors(a.v, a.v_s, s.v_width);
+  const AttendPick pick = attend_pick(op, s, vec, q.scratch ? q.scratch_bytes : 0);
+  a.m = p.m; a.n = p.n; a.share = (int32_t)s.share; a.width = q.width; a.v_width = (int32_t)s.v_width;
+  a.batch = (int32_t)s.batch;
+  a.causal = (p.flags & OPARA_FLAG_CAUSAL) ? 1 : (p.flags & OPARA_FLAG_CAUSAL_END) ? 2 : 0;
+  a.first = q.first;
+  a.scale = p.alpha * 1.44269504088896341f;
+  a.tiles = (int32_t)pick.tiles;
+  a.splits = (int32_t)pick.splits;
+  if (a.splits > 1) {
+    a.counters = (uint32_t *)q.scratch;
+    a.partials = (float *)((unsigned char *)q.scratch + pick.counter_bytes);
+  }
+  a.div_share = div_magic(s.share);
+  a.div_splits = div_magic(a.splits);
+  out->kernel = vec ? pick.form->kernel : pick.form->any;
+  const int64_t gx = pick.tiles * pick.splits;
   if (gx * s.kv_heads * s.batch > kInt) return too_large("more rows than one launch holds", op);
-  out->gx = (uint32_t)gx; out->gy = (uint32_t)s.kv_heads; out->gz = (uint32_t)s.batch; out->block = 256;
+  out->gx = (uint32_t)gx; out->gy = (uint32_t)s.kv_heads; out->gz = (uint32_t)s.batch; out->block = (uint32_t)pick.form->threads;
   out->args.attend = a;
   return OPARA_OK;
 }
@@ -314,6 +356,8 @@ extern "C" int opara_scratch_bytes(const opara_op_desc *op, const opara_op_more 
   if (op->op_type != OPARA_ATTENTION) return OPARA_OK;
   AttendShape s;
   const int rc = attend_shape(*op, more ? *more : opara_op_more{}, &s);
-  if (rc == OPARA_OK) *bytes = (uint64_t)s.scratch;
-  return rc;
+  if (rc != OPARA_OK) return rc;
+  // Whether keys and values are aligned shows later: enough for either case.
+  for (bool vec : {false, true}) *bytes = std::max<uint64_t>(*bytes, (uint64_t)attend_pick(*op, s, vec, UINT64_MAX).scratch);
+  return OPARA_OK;
 }

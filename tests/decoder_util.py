@@ -22,6 +22,38 @@ GATED = [(1, 8, 1), (1, 64, 33), (2, 768, 2048), (3, 1027, 100), (4, 4096, 512),
          (64, 64, 64), (77, 768, 2048), (128, 1024, 768), (130, 200, 72), (257, 512, 520), (300, 33, 257), (512, 2048, 1024),
          (300, 1024, 2100), (520, 512, 4100), (1000, 640, 4000), (2040, 1032, 4090), (256, 264, 4092)]
 
+# batch, m, n, heads, kv_heads, width, v_width, lengths, causal, first
+ATTEND = [
+    (1, 1, 1, 1, 1, 8, 8, None, None, 0),
+    (1, 1, 1500, 12, 12, 64, 64, None, None, 0),
+    (1, 1, 5000, 8, 2, 128, 128, None, None, 0),
+    (1, 3, 4099, 6, 1, 64, 128, None, "end", 0),
+    (4, 77, 130, 4, 4, 64, 64, [130, 1, 0, 77], None, 0),
+    (3, 20, 50, 6, 2, 32, 48, [-5, 99, 13], "end", 0),
+    (1, 128, 128, 2, 1, 128, 128, None, "start", 0),
+    (2, 65, 65, 3, 3, 40, 40, None, "start", 0),
+    (1, 30, 90, 2, 2, 64, 64, None, "start", 60),
+    (1, 30, 90, 2, 2, 64, 64, None, "start", -10),
+    (1, 5, 33, 2, 1, 20, 24, None, None, 0),
+    (2, 9, 70, 2, 2, 37, 19, [70, 31], "end", 0),
+    (1, 50, 300, 1, 1, 256, 256, None, None, 0),
+    (1, 2, 3000, 4, 4, 200, 72, None, "start", 2998),
+    (1, 16, 31, 7, 1, 96, 96, None, None, 0),
+    (1, 200, 515, 8, 4, 128, 128, [515], "end", 0),
+    (2, 300, 300, 4, 2, 64, 64, [300, 201], "start", 0),
+    (1, 513, 257, 2, 2, 128, 64, None, "end", 0),
+    (1, 1, 20000, 1, 1, 64, 64, None, None, 0),
+    (1, 12, 150, 1, 1, 130, 30, None, None, 0),
+    (1, 700, 2100, 4, 1, 64, 64, [2077], "end", 0),
+    (1, 1000, 1000, 8, 8, 128, 128, None, "start", 0),
+    (2, 700, 130, 8, 8, 128, 96, [101, 130], None, 0),
+    (1, 1000, 130, 8, 8, 48, 64, None, "end", 0),
+    (2, 333, 1111, 12, 12, 64, 40, [1111, 5], None, 0),
+    (3, 1500, 400, 24, 8, 96, 128, [400, 0, 77], None, 0),
+    (2, 40, 300, 4, 2, 101, 77, [300, 222], "end", 0),
+    (1, 300, 12000, 7, 1, 128, 128, None, "start", 11650),
+]
+
 
 def normal(gen, shape, dtype, std=1.0, mean=0.0):
     return (torch.randn(shape, generator=gen, dtype=torch.float64) * std + mean).to(TORCH[dtype])

@@ -6,7 +6,7 @@ from fractions import Fraction
 import numpy as np
 import pytest
 
-from decoder_util import GATED as GATED_SIZES, build, describe
+from decoder_util import ATTEND as ATTEND_SIZES, GATED as GATED_SIZES, build, describe
 from oracle import executor, ops as O
 from paper_2312_10351_amd import binding as B
 from paper_2312_10351_amd.runtime import Session
@@ -196,6 +196,21 @@ def test_gated_sizes_of_the_gpu_tests_reach_every_form():
         all_of_them = {B.opara_kernel_info(i)[0] for i in range(B.opara_kernel_count())}
         taken = {build(describe(B.GATED, dtype, 1, m=m, n=n, k=k, weight=0x2000))[0] for m, k, n in GATED_SIZES}
         assert taken == {name for name in all_of_them if name.startswith(f"gated_{dtype}_")}
+
+
+def test_attention_sizes_of_the_gpu_tests_reach_every_form():
+    every = [B.opara_kernel_info(i)[0] for i in range(B.opara_kernel_count())]
+    for dtype in ("f16", "f32"):
+        taken = {}
+        for batch, m, n, heads, kv, width, v_width, _, causal, first in ATTEND_SIZES:
+            op = describe(B.ATTENTION, dtype, 3, batch=batch, m=m, n=n, heads=heads, kv_heads=kv, width=width, v_width=v_width,
+                          first=first, alpha=1.0, flags={None: 0, "start": B.FLAG_CAUSAL, "end": B.FLAG_CAUSAL_END}[causal])
+            op[1].scratch_bytes = B.opara_scratch_bytes(*op)
+            op[1].scratch = 0x900000 if op[1].scratch_bytes else None
+            taken.setdefault(build(op)[0], set()).add(op[1].scratch_bytes > 0)
+        assert set(taken) == {name for name in every if name.startswith(f"attend_{dtype}_")}
+        for name in ("rows64", "rows128") + (("wide64", "wide128") if dtype == "f16" else ()):
+            assert taken[f"attend_{dtype}_{name}"] == {False, True}, name
 
 
 # ---- in a DAG ------------------------------------------------------------------------------

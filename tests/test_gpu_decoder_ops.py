@@ -183,34 +183,10 @@ def test_gated_rows_apart_unaligned_and_without_bias(dtype, m, k, n, lda, ldy, l
 
 # ---- attention -----------------------------------------------------------------------------
 
-# batch, m, n, heads, kv_heads, width, v_width, lengths, causal, first
-ATTEND = [
-    (1, 1, 1, 1, 1, 8, 8, None, None, 0),
-    (1, 1, 1500, 12, 12, 64, 64, None, None, 0),
-    (1, 1, 5000, 8, 2, 128, 128, None, None, 0),
-    (1, 3, 4099, 6, 1, 64, 128, None, "end", 0),
-    (4, 77, 130, 4, 4, 64, 64, [130, 1, 0, 77], None, 0),
-    (3, 20, 50, 6, 2, 32, 48, [-5, 99, 13], "end", 0),
-    (1, 128, 128, 2, 1, 128, 128, None, "start", 0),
-    (2, 65, 65, 3, 3, 40, 40, None, "start", 0),
-    (1, 30, 90, 2, 2, 64, 64, None, "start", 60),
-    (1, 30, 90, 2, 2, 64, 64, None, "start", -10),
-    (1, 5, 33, 2, 1, 20, 24, None, None, 0),
-    (2, 9, 70, 2, 2, 37, 19, [70, 31], "end", 0),
-    (1, 50, 300, 1, 1, 256, 256, None, None, 0),
-    (1, 2, 3000, 4, 4, 200, 72, None, "start", 2998),
-    (1, 16, 31, 7, 1, 96, 96, None, None, 0),
-    (1, 200, 515, 8, 4, 128, 128, [515], "end", 0),
-    (2, 300, 300, 4, 2, 64, 64, [300, 201], "start", 0),
-    (1, 513, 257, 2, 2, 128, 64, None, "end", 0),
-    (1, 1, 20000, 1, 1, 64, 64, None, None, 0),
-]
-
-
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
-@pytest.mark.parametrize("i", range(len(ATTEND)))
+@pytest.mark.parametrize("i", range(len(D.ATTEND)))
 def test_attention(dtype, i):
-    batch, m, n, heads, kv, width, v_width, lengths, causal, first = ATTEND[i]
+    batch, m, n, heads, kv, width, v_width, lengths, causal, first = D.ATTEND[i]
     g = gen(i)
     q, k, v = (D.normal(g, s, dtype) for s in [(batch * m, heads * width), (batch * n, kv * width), (batch * n, kv * v_width)])
     ext = [q, k, v]
@@ -257,7 +233,7 @@ def test_attention_through_strides(dtype, m, n, scratch):
                [m * (width + 16), width + 16, batch * m * (width + 16)]]
     d = D.describe(B.ATTENTION, dtype, 3, batch=batch, m=m, n=n, heads=heads, kv_heads=kv, width=width, alpha=0.125, strides=strides, out=y.data_ptr())
     d[1].scratch_bytes = B.opara_scratch_bytes(*d)
-    assert (d[1].scratch_bytes > 0) == (m == 1)
+    assert d[1].scratch_bytes > 0 or m > 1
     room = torch.zeros(max(d[1].scratch_bytes, 256), dtype=torch.uint8, device=DEV)
     d[1].scratch = room.data_ptr() if scratch else None
     eager(d, [qd, both, both[..., width:]], dtype)
