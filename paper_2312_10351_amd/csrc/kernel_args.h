@@ -203,9 +203,17 @@ struct AttendArgs {
   X(rotary_f32, RotaryArgs)             \
   X(resnorm_f16_wave, NormArgs)         \
   X(resnorm_f16_block, NormArgs)        \
+  X(resnorm_f16_large, NormArgs)        \
+  X(resnorm_f16_huge, NormArgs)         \
+  X(resnorm_f16_odd, NormArgs)          \
+  X(resnorm_f16_oddlarge, NormArgs)     \
   X(resnorm_f16_wide, NormArgs)         \
   X(resnorm_f32_wave, NormArgs)         \
   X(resnorm_f32_block, NormArgs)        \
+  X(resnorm_f32_large, NormArgs)        \
+  X(resnorm_f32_huge, NormArgs)         \
+  X(resnorm_f32_odd, NormArgs)          \
+  X(resnorm_f32_oddlarge, NormArgs)     \
   X(resnorm_f32_wide, NormArgs)         \
   X(gated_f16_any, IgemmArgs)           \
   X(gated_f16_row, IgemmArgs)          \
@@ -335,7 +343,8 @@ constexpr int kRowCacheChunks = 4;    // 16-byte chunks a thread keeps in regist
 constexpr int kAttnMaxCols = 512;     // attention kernel: one 16-byte chunk of scores per lane of a wavefront
 constexpr int kAttnMaxWidth = 64;     // ... one 128-byte line per row of q, k and v
 constexpr int kGemvMaxM = 4;
-constexpr int kNormWaveChunks = 2, kNormBlockChunks = 8;   // 16-byte chunks a thread of the residual norm keeps
+// What a thread of the residual norm keeps of a row: 16-byte pieces, or elements where rows are not made of them.
+constexpr int kNormWavePieces = 2, kNormBlockPieces = 2, kNormLargePieces = 4, kNormHugePieces = 8, kNormOddPieces = 8;
 constexpr int kGatedRowMaxCols = 1024;                    // one row: up to here a wavefront per column
 constexpr int kGatedAnyRows = 64, kGatedAnyCols = 32;      // tile of the gated block's general form
 constexpr int kAttendRows = 16;       // query rows per workgroup

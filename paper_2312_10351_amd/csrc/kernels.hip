@@ -1642,16 +1642,21 @@ KDEFT(igemm_f32_quad4s_tail, 256, 3, lds_split(1, 1, 3), IgemmArgs, (igemm_split
 
 KDEF2(attention_f16, 256, 2, kLdsAttention, AttnArgs, (attention_body(a, b, lds)))
 
-// The blocks of a decoder.
+// The blocks of a decoder: X(kernel name, argument record, wavefronts per SIMD, body call).
 #define DECODER_BODIES(X, T, tn)                                                                              \
-  X(rotary_##tn, RotaryArgs, (rotary_body<T>(a, b, lds)))                                                     \
-  X(resnorm_##tn##_wave, NormArgs, (residual_norm_body<T, 64, kNormWaveChunks>(a, b, lds)))                   \
-  X(resnorm_##tn##_block, NormArgs, (residual_norm_body<T, 256, kNormBlockChunks>(a, b, lds)))                \
-  X(resnorm_##tn##_wide, NormArgs, (residual_norm_wide_body<T>(a, b, lds)))
-#define KDECODER(name, Args, call) KDEF(name, 256, kLdsRow, Args, call)
+  X(rotary_##tn, RotaryArgs, 4, (rotary_body<T>(a, b, lds)))                                                  \
+  X(resnorm_##tn##_wave, NormArgs, 4, (residual_norm_body<T, 64, kNormWavePieces, Vec16<T>::N, true>(a, b, lds)))     \
+  X(resnorm_##tn##_block, NormArgs, 4, (residual_norm_body<T, 256, kNormBlockPieces, Vec16<T>::N, true>(a, b, lds)))  \
+  X(resnorm_##tn##_large, NormArgs, 2, (residual_norm_body<T, 256, kNormLargePieces, Vec16<T>::N, false>(a, b, lds))) \
+  X(resnorm_##tn##_odd, NormArgs, 4, (residual_norm_body<T, 256, kNormOddPieces, 1, true>(a, b, lds)))        \
+  X(resnorm_##tn##_oddlarge, NormArgs, 4, (residual_norm_body<T, 256, 2 * kNormOddPieces, 1, false>(a, b, lds))) \
+  X(resnorm_##tn##_wide, NormArgs, 4, (residual_norm_wide_body<T>(a, b, lds)))
+#define KDECODER(name, Args, waves, call) KDEF2(name, 256, waves, kLdsRow, Args, call)
 DECODER_BODIES(KDECODER, half_t, f16)
 DECODER_BODIES(KDECODER, float, f32)
 #undef KDECODER
+KDEF2(resnorm_f16_huge, 256, 1, kLdsRow, NormArgs, (residual_norm_body<half_t, 256, kNormHugePieces, 8, false>(a, b, lds)))
+KDEF2(resnorm_f32_huge, 256, 2, kLdsRow, NormArgs, (residual_norm_body<float, 256, kNormHugePieces, 4, false>(a, b, lds)))
 KDEF(gated_f16_any, 256, kLdsGatedAny, IgemmArgs, (gated_any_body<half_t>(a, b, lds)))
 KDEF(gated_f32_any, 256, kLdsGatedAny, IgemmArgs, (gated_any_body<float>(a, b, lds)))
 KDEF2(gated_f16_tile256, 512, 2, lds_tile(256, 256, 2), IgemmArgs, (gated_wide_body<256, 256, 4, 2>(a, b, lds)))
@@ -2044,12 +2049,13 @@ __device__ __forceinline__ void group_body() {
     CA &a = *(CA *)&ga.args[i];                               \
     call;                                                     \
   } break;
+#define GCASE4(name, Args, waves, call) GCASE(name, Args, call)
   if constexpr (FLAVOR == 3) {
     typedef typename std::conditional<F16, half_t, float>::type T;
     if constexpr (F16) {
-      switch (me.kernel) { DECODER_BODIES(GCASE, T, f16) default: break; }
+      switch (me.kernel) { DECODER_BODIES(GCASE4, T, f16) default: break; }
     } else {
-      switch (me.kernel) { DECODER_BODIES(GCASE, T, f32) default: break; }
+      switch (me.kernel) { DECODER_BODIES(GCASE4, T, f32) default: break; }
     }
   } else if constexpr (F16) {
     switch (me.kernel) {
@@ -2092,6 +2098,7 @@ __device__ __forceinline__ void group_body() {
         break;
     }
   }
+#undef GCASE4
 #undef GCASE
   if constexpr (TRACE) op_trace_end(ga.trace, tag, t0, (unsigned)tile, (unsigned)me.tiles);
 }
@@ -2387,6 +2394,8 @@ int group_flavor(int id) {
 #define FCASE(name, Args, call) case K_##name:
     HEAVY_BODIES(FCASE, half_t, f16, 0) HEAVY_BODIES(FCASE, float, f32, 0) FAR_BODIES(FCASE, half_t, f16, 0) FAR_BODIES(FCASE, float, f32, 0) return 2;
     LIGHT_BODIES(FCASE, half_t, f16, 0) LIGHT_BODIES(FCASE, float, f32, 0) return 1;
+#undef FCASE
+#define FCASE(name, Args, waves, call) case K_##name:
     DECODER_BODIES(FCASE, half_t, f16) DECODER_BODIES(FCASE, float, f32) return kGroupDecoder;
 #undef FCASE
     default: return id >= 0 && id < K_attention_f16 ? 0 : -1;     // merged operators run as launches of their own

@@ -81,12 +81,21 @@ int plan_norm(const opara_op_desc &op, const opara_op_more &q, const void *const
   a.div_gate = div_magic(a.gate_rows);
   a.rms = (p.flags & OPARA_FLAG_RMS) ? 1 : 0;
   a.after = after; a.before = before;
-  a.eps = p.eps; a.alpha = p.alpha; a.beta = q.beta;
-  static const int ids[2][3] = {{K_resnorm_f32_wave, K_resnorm_f32_block, K_resnorm_f32_wide},
-                                {K_resnorm_f16_wave, K_resnorm_f16_block, K_resnorm_f16_wide}};
-  const int form = p.n <= 64 * ve * kNormWaveChunks ? 0 : p.n <= 256 * ve * kNormBlockChunks ? 1 : 2;
+  a.eps = p.eps; a.alpha = a.r ? p.alpha : 0.f; a.beta = q.beta;
+  const bool vec = p.n % ve == 0 && aligned16(a.x) && aligned16(a.r) && aligned16(a.g) && aligned16(a.w) && aligned16(a.b) && aligned16(a.y) &&
+                   aligned16(a.s);
+  enum { kWave, kBlock, kLarge, kHuge, kOdd, kOddLarge, kWide };
+  static const int ids[2][7] = {
+      {K_resnorm_f32_wave, K_resnorm_f32_block, K_resnorm_f32_large, K_resnorm_f32_huge, K_resnorm_f32_odd, K_resnorm_f32_oddlarge, K_resnorm_f32_wide},
+      {K_resnorm_f16_wave, K_resnorm_f16_block, K_resnorm_f16_large, K_resnorm_f16_huge, K_resnorm_f16_odd, K_resnorm_f16_oddlarge, K_resnorm_f16_wide}};
+  int form = kWide;
+  if (vec) form = p.n <= 64 * ve * kNormWavePieces ? kWave : p.n <= 256 * ve * kNormBlockPieces ? kBlock
+                : p.n <= 256 * ve * kNormLargePieces ? kLarge : p.n <= 256 * ve * kNormHugePieces ? kHuge : kWide;
+  else form = p.n <= 256 * kNormOddPieces ? kOdd : p.n <= 512 * kNormOddPieces ? kOddLarge : kWide;
   out->kernel = ids[f16][form];
-  out->gx = form == 0 ? (uint32_t)cdiv(p.m, 4) : (uint32_t)p.m;
+  // Workgroups that the chip holds at once; with more rows than that a workgroup takes several.
+  static const int64_t resident[7] = {1024, 1024, 512, 256, 1024, 1024, kInt};
+  out->gx = (uint32_t)std::min(form == kWave ? cdiv(p.m, 4) : (int64_t)p.m, resident[form]);
   out->gy = out->gz = 1; out->block = 256;
   out->args.norm = a;
   return OPARA_OK;

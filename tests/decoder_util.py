@@ -17,6 +17,9 @@ TINY = {"f16": 2.0 ** -25, "f32": 2.0 ** -149}
 TORCH = {"f16": torch.float16, "f32": torch.float32}
 
 
+# rows, columns of residual norms that take every form
+NORM = [(1, 1), (1, 768), (5, 1024), (3, 1027), (77, 33), (4, 4096), (2, 8200), (3, 16384), (2, 16385), (1, 20011), (2, 2051), (3, 6000),
+        (4300, 40), (1100, 2056), (2100, 7)]
 # rows, K, columns of gated blocks that take every form the planner has
 GATED = [(1, 8, 1), (1, 64, 33), (2, 768, 2048), (3, 1027, 100), (4, 4096, 512), (5, 256, 96), (16, 512, 130), (17, 40, 31), (33, 320, 640),
          (64, 64, 64), (77, 768, 2048), (128, 1024, 768), (130, 200, 72), (257, 512, 520), (300, 33, 257), (512, 2048, 1024),

@@ -6,7 +6,7 @@ from fractions import Fraction
 import numpy as np
 import pytest
 
-from decoder_util import ATTEND as ATTEND_SIZES, GATED as GATED_SIZES, build, describe
+from decoder_util import ATTEND as ATTEND_SIZES, GATED as GATED_SIZES, NORM as NORM_SIZES, build, describe
 from oracle import executor, ops as O
 from paper_2312_10351_amd import binding as B
 from paper_2312_10351_amd.runtime import Session
@@ -189,6 +189,13 @@ def test_scratch_is_asked_for_where_keys_are_shared_out():
     for more in (few[1], None):
         with pytest.raises(B.OparaError):
             B.opara_scratch_bytes(few[0], more)
+
+
+def test_norm_sizes_of_the_gpu_tests_reach_every_form():
+    every = [B.opara_kernel_info(i)[0] for i in range(B.opara_kernel_count())]
+    for dtype in ("f16", "f32"):
+        taken = {build(describe(B.RESIDUAL_NORM, dtype, 2, **{**NORM, "m": m, "n": n}))[0] for m, n in NORM_SIZES}
+        assert taken == {name for name in every if name.startswith(f"resnorm_{dtype}_")}
 
 
 def test_gated_sizes_of_the_gpu_tests_reach_every_form():

@@ -89,7 +89,7 @@ def test_rotary_rows_apart_and_unaligned(dtype, lead, pitch):
 # ---- the norms around a residual sum ------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
-@pytest.mark.parametrize("m, n", [(1, 1), (1, 768), (5, 1024), (3, 1027), (77, 33), (4, 4096), (2, 8200), (3, 16384), (2, 16385), (1, 20011)])
+@pytest.mark.parametrize("m, n", D.NORM)
 @pytest.mark.parametrize("rms, after, before, gates", [(True, False, True, 0), (False, True, True, 1), (True, True, False, -1), (False, False, True, -1)])
 def test_residual_norm(dtype, m, n, rms, after, before, gates):
     g = gen(m * n + after)
