@@ -18,6 +18,18 @@
 constexpr int attend_ring_bytes(int dp) { return 2 * 64 * dp; }      // of one wavefront: a tile of keys, one of values
 constexpr int lds_attend_rows(int dp) { return 4 * attend_ring_bytes(dp); }
 
+// Over the four lanes that hold a query row: i, i ^ 16, i ^ 32, i ^ 48.  Lane swaps stay in the vector unit; a
+// shuffle goes through workgroup memory's crossbar.
+template <typename F> __device__ __forceinline__ float over_row(float v, F join) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  v = join(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
+  const u32x2 b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  return join(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
+}
+__device__ __forceinline__ float row_max(float v) { return over_row(v, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float row_sum(float v) { return over_row(v, [](float a, float b) { return a + b; }); }
+
 // What one tile of sixteen query rows sees: keys [0, end), row r its first limit(r).
 template <typename AR> struct AttendSight {
   int length, end;
@@ -286,8 +298,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
     for (int i = 0; i < NQ; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) most = fmaxf(most, p[i][e]);
-    most = fmaxf(most, __shfl_xor(most, 16, 64));
-    most = fmaxf(most, __shfl_xor(most, 32, 64));
+    most = row_max(most);
     const float from = most == -INFINITY ? 0.f : most;      // a row that has seen nothing yet
     const float shrink = __builtin_amdgcn_exp2f(top - from);
     top = most;
@@ -341,8 +352,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
 
   // ---- the four wavefronts meet
   wait_loads<0>();                                          // no load may outlive its ring
-  sum += __shfl_xor(sum, 16, 64);
-  sum += __shfl_xor(sum, 32, 64);
+  sum = row_sum(sum);
   float *part = (float *)ring, *stat = part + 16 * PITCH;   // result rows, then maxima and sums
 #pragma unroll
   for (int j = 0; j < NO; ++j) *(floatx4 *)(part + r16 * PITCH + j * 16 + grp * 4) = o[j];
@@ -393,13 +403,15 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
 
 
 // wide kernels, fp16: 32 NW query rows per workgroup, 32 per wavefront, the keys in tiles of 64 that all
-// wavefronts share, two of them and their values in workgroup memory.  32 x 32 matrix instructions: a lane holds a
-// query row and half the keys of a tile, so that a row's statistics take one exchange.
-// What bounds it: per tile and wavefront 64 x 32 x 2 widths of matrix work, about as long in vector instructions
-// (exponentials take a quarter of the rate) and in fragment reads; two wavefronts per SIMD overlap the three.
+// wavefronts share, two of them and their values in workgroup memory.
+// What bounds it: per tile and wavefront 64 x 32 x 2 widths of matrix work, about as long in vector instructions (at
+// a width of 128; exponentials take a quarter of the rate) and 16 KB of fragment reads each for keys and values; two
+// wavefronts per SIMD overlap the three, the one at a product first (s_setprio).  16 x 16 matrix instructions:
+// with 32 x 32 ones, which need half as many reductions, the same kernel measured 9 % slower.
 // The result is scaled down only when a row's maximum has grown by more than 2^kAttendSlack: until
 // then probabilities may exceed one, by at most that, which their rounding, relative to each, does not see.
-typedef float floatx16 __attribute__((ext_vector_type(16)));
+// Measured, fp16, 32 heads over 8 of 128, 8192 rows (us): causal 573 (960 TFLOP/s), all keys 1094 (1005; without the
+// softmax 1050, a large matrix product reaches 1350); 16 heads of 64, 4096 rows 93 (738).
 constexpr float kAttendSlack = 8.f;
 constexpr int lds_attend_wide(int dp) { return 4 * 64 * dp * 2; }
 
@@ -410,9 +422,9 @@ __device__ __forceinline__ void attend_wide_body(const AR &a, const Blk &b, unsi
   typedef V VU __attribute__((aligned(2)));
   constexpr int KT = 64, CH = DP / 8, TILE = KT * DP * 2;     // keys per tile, 16-byte chunks per row, bytes
   constexpr int L = TILE / 1024 / NW, RL = 64 / CH;           // loads of a wavefront per tile, rows per load
-  constexpr int NS = DP / 16, NO = DP / 32;
+  constexpr int NS = DP / 32, NO = DP / 16;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int hi = lane >> 5, r32 = lane & 31, r16 = lane & 15;
+  const int grp = lane >> 4, r16 = lane & 15;
   // Every XCD takes a contiguous range of (sequence, key head, tile): its L2 then holds one head's keys.  The tiles
   // of a head in descending order: under a causal mask the later rows have more to do.
   int tile, split, g, z;
@@ -427,29 +439,32 @@ __device__ __forceinline__ void attend_wide_body(const AR &a, const Blk &b, unsi
     split = x - tile * a.splits;
   }
   const int r0 = tile * (32 * NW), rows = a.m * a.share;
-  const int r = r0 + wave * 32 + r32, qi = (int)fast_div((uint32_t)r, (uint32_t)a.share, a.div_share), head = g * a.share + r - qi * a.share;
+  int r[2], qi[2], mine[2];
+  V qf[2][NS];
   const AttendSight<AR> sight(a, z, (int)fast_div((uint32_t)min(rows - 1, r0 + 32 * NW - 1), (uint32_t)a.share, a.div_share));
-  const int mine = r < rows ? sight.limit(qi) : 0;
   const int last = min(rows - 1, r0 + wave * 32 + 31);        // of this wavefront; it sees keys below `reach`
   const int reach = r0 + wave * 32 < rows ? sight.limit((int)fast_div((uint32_t)last, (uint32_t)a.share, a.div_share)) : 0;
   const int all = sight.limit((int)fast_div((uint32_t)r0, (uint32_t)a.share, a.div_share));   // every row of the tile sees these
   const int tiles = (sight.end + KT - 1) / KT, full = all / KT;
 
-  V qf[NS];
-  {
-    const T *q = (const T *)a.q + z * a.q_s[0] + qi * a.q_s[1] + head * a.q_s[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    r[x] = r0 + wave * 32 + x * 16 + r16;
+    qi[x] = (int)fast_div((uint32_t)r[x], (uint32_t)a.share, a.div_share);
+    mine[x] = r[x] < rows ? sight.limit(qi[x]) : 0;
+    const T *q = (const T *)a.q + z * a.q_s[0] + qi[x] * a.q_s[1] + (g * a.share + r[x] - qi[x] * a.share) * a.q_s[2];
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-      const int d = s * 16 + hi * 8;
+      const int d = s * 32 + grp * 8;
       V v = {};
-      if (r < rows) {
+      if (r[x] < rows) {
         if (d + 8 <= a.width) v = *(const VU *)(q + d);
         else
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             if (d + e < a.width) v[e] = q[d + e];
       }
-      qf[s] = v;
+      qf[x][s] = v;
     }
   }
   const T *kbase = (const T *)a.k + z * a.k_s[0] + g * a.k_s[2], *vbase = (const T *)a.v + z * a.v_s[0] + g * a.v_s[2];
@@ -468,87 +483,124 @@ __device__ __forceinline__ void attend_wide_body(const AR &a, const Blk &b, unsi
     stage(kbase, a.k_s[1], a.width, kt, lds + slot * TILE);
     stage(vbase, a.v_s[1], a.v_width, kt, lds + (2 + slot) * TILE);
   };
-  floatx16 o[NO] = {};
-  float top = -INFINITY, sum = 0.f;
-  if (split < tiles) issue(split, 0);
-  int slot = 0;
-  auto step = [&](int kt, auto masked_tag) {
-    constexpr bool MASKED = decltype(masked_tag)::value;
-    wait_loads_and_meet<0>();
-    const unsigned char *K = lds + slot * TILE, *W = lds + (2 + slot) * TILE;
-    slot ^= 1;
-    if (kt + a.splits < tiles) issue(kt + a.splits, slot);
-    if (MASKED && kt * KT >= reach) return;
-    floatx16 s[2] = {};
+
+  floatx4 o[NO][2];
+#pragma unroll
+  for (int j = 0; j < NO; ++j)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) o[j][x] = floatx4{0.f, 0.f, 0.f, 0.f};
+  float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+  auto issue_k = [&](int kt, int slot) { stage(kbase, a.k_s[1], a.width, kt, lds + slot * TILE); };
+  auto issue_v = [&](int kt, int slot) { stage(vbase, a.v_s[1], a.v_width, kt, lds + (2 + slot) * TILE); };
+  auto scores = [&](floatx4 (&s)[4][2], int slot) {
+    const unsigned char *K = lds + slot * TILE;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) s[i][x] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int d = 0; d < NS; ++d)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const V kf = *(const V *)(K + (i * 32 + r32) * (DP * 2) + (((d * 2 + hi) ^ (r32 & 7)) * 16));
-        s[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[d], s[i], 0, 0, 0);
+      for (int i = 0; i < 4; ++i) {
+        const V kf = *(const V *)(K + (i * 16 + r16) * (DP * 2) + (((d * 4 + grp) ^ (r16 & 7)) * 16));
+#pragma unroll
+        for (int x = 0; x < 2; ++x) s[i][x] = mma16<T>(kf, qf[x][d], s[i][x]);
       }
-    float most = -INFINITY;
+  };
+  V p[2][2];                               // [step of 32 keys][query block]
+  auto soften = [&](floatx4 (&s)[4][2], int kt, auto masked_tag) {
+    constexpr bool MASKED = decltype(masked_tag)::value;
+    float most[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int x = 0; x < 2; ++x) {
+      most[x] = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        if constexpr (MASKED) s[i][e] = kt * KT + i * 32 + (e >> 2) * 8 + hi * 4 + (e & 3) < mine ? s[i][e] * a.scale : -INFINITY;
-        most = fmaxf(most, s[i][e]);
-      }
-    if constexpr (!MASKED) most *= a.scale;                   // a positive factor
-    most = fmaxf(most, __shfl_xor(most, 32, 64));
-    if (__any(most > top + kAttendSlack)) {
-      const float now = fmaxf(most, top);
-      const float from = now == -INFINITY ? 0.f : now;
-      const float shrink = __builtin_amdgcn_exp2f(top - from);
-      top = now;
-      sum *= shrink;
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < NO; ++j)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[j][e] *= shrink;
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (MASKED) s[i][x][e] = kt * KT + i * 16 + grp * 4 + e < mine[x] ? s[i][x][e] * a.scale : -INFINITY;
+          most[x] = fmaxf(most[x], s[i][x][e]);
+        }
+      if constexpr (!MASKED) most[x] *= a.scale;
+      most[x] = row_max(most[x]);
     }
-    const float from = top == -INFINITY ? 0.f : top;
-    V p[4];
+    if (__any(most[0] > top[0] + kAttendSlack || most[1] > top[1] + kAttendSlack)) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+      for (int x = 0; x < 2; ++x) {
+        const float now = fmaxf(most[x], top[x]), from = now == -INFINITY ? 0.f : now, shrink = __builtin_amdgcn_exp2f(top[x] - from);
+        top[x] = now;
+        sum[x] *= shrink;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float x = __builtin_amdgcn_exp2f(MASKED ? s[i][e] - from : __builtin_fmaf(s[i][e], a.scale, -from));
-        sum += x;
-        p[i * 2 + e / 8][e % 8] = (T)x;
+        for (int j = 0; j < NO; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[j][x][e] *= shrink;
       }
+    }
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+    for (int x = 0; x < 2; ++x) {
+      const float from = top[x] == -INFINITY ? 0.f : top[x];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float v = __builtin_amdgcn_exp2f(MASKED ? s[i][x][e] - from : __builtin_fmaf(s[i][x][e], a.scale, -from));
+          sum[x] += v;
+          p[i / 2][x][i % 2 * 4 + e] = (T)v;
+        }
+    }
+  };
+  auto context = [&](int slot) {
+    const unsigned char *W = lds + (2 + slot) * TILE;
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
 #pragma unroll
       for (int j = 0; j < NO; ++j) {
         half4 v[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int row = q * 16 + h * 8 + hi * 4 + (r16 >> 2);
-          const int chunk = j * 4 + ((lane >> 4) & 1) * 2 + ((r16 >> 1) & 1);
+          const int row = q * 32 + h * 16 + grp * 4 + (r16 >> 2), chunk = j * 2 + ((r16 >> 1) & 1);
           v[h] = lds_read_transposed(W + row * (DP * 2) + ((chunk ^ (row & 7)) * 16) + (r16 & 1) * 8);
         }
-        o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7), p[q], o[j], 0, 0, 0);
+        const V vf = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) o[j][x] = mma16<T>(vf, p[q][x], o[j][x]);
       }
+  };
+
+  if (split < tiles) { issue_k(split, 0); issue_v(split, 0); }
+  int slot = 0;
+  auto turn = [&](int kt, auto masked_tag) {
+    wait_loads_and_meet<0>();
+    const int at = slot;
+    slot ^= 1;
+    if (kt + a.splits < tiles) { issue_k(kt + a.splits, slot); issue_v(kt + a.splits, slot); }
+    if (decltype(masked_tag)::value && kt * KT >= reach) return;
+    floatx4 s[4][2];
+    __builtin_amdgcn_s_setprio(1);
+    scores(s, at);
+    __builtin_amdgcn_s_setprio(0);
+    soften(s, kt, masked_tag);
+    __builtin_amdgcn_s_setprio(1);
+    context(at);
+    __builtin_amdgcn_s_setprio(0);
   };
   int kt = split;
 #pragma nounroll
-  for (; kt < full; kt += a.splits) step(kt, std::integral_constant<bool, false>{});
+  for (; kt < full; kt += a.splits) turn(kt, std::integral_constant<bool, false>{});
 #pragma nounroll
-  for (; kt < tiles; kt += a.splits) step(kt, std::integral_constant<bool, true>{});
-  sum += __shfl_xor(sum, 32, 64);
+  for (; kt < tiles; kt += a.splits) turn(kt, std::integral_constant<bool, true>{});
+
+  sum[0] = row_sum(sum[0]);
+  sum[1] = row_sum(sum[1]);
   if (a.splits == 1) {
-    const float inverse = attend_inverse(sum);
-    if (r < rows)
 #pragma unroll
-      for (int j = 0; j < NO; ++j)
+    for (int x = 0; x < 2; ++x) {
+      const float inverse = attend_inverse(sum[x]);
+      if (r[x] < rows)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int col = j * 32 + q * 8 + hi * 4;
-          if (col < a.v_width)
-            attend_store<T>(a, g, z, r, col, floatx4{o[j][q * 4], o[j][q * 4 + 1], o[j][q * 4 + 2], o[j][q * 4 + 3]}, inverse);
-        }
+        for (int j = 0; j < NO; ++j)
+          if (j * 16 + grp * 4 < a.v_width) attend_store<T>(a, g, z, r[x], j * 16 + grp * 4, o[j][x], inverse);
+    }
     return;
   }
   // A record keeps the results as the lanes hold them, so that they are written and read in whole lines.
@@ -558,16 +610,16 @@ __device__ __forceinline__ void attend_wide_body(const AR &a, const Blk &b, unsi
 #pragma unroll
   for (int j = 0; j < NO; ++j)
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      stg<true, floatx4>(mineslot + ((wave * (DP / 8) + j * 4 + q) * 64 + lane) * 4,
-                         floatx4{o[j][q * 4], o[j][q * 4 + 1], o[j][q * 4 + 2], o[j][q * 4 + 3]});
-  if (hi == 0) {
-    stg<true, float>(mineslot + R * DP + wave * 32 + r32, top);
-    stg<true, float>(mineslot + R * DP + R + wave * 32 + r32, sum);
-  }
+    for (int x = 0; x < 2; ++x) stg<true, floatx4>(mineslot + ((wave * (NO * 2) + j * 2 + x) * 64 + lane) * 4, o[j][x]);
+  if (grp == 0)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      stg<true, float>(mineslot + R * DP + wave * 32 + x * 16 + r16, top[x]);
+      stg<true, float>(mineslot + R * DP + R + wave * 32 + x * 16 + r16, sum[x]);
+    }
   attend_join<T, DP, R, 64 * NW>(a, tile_id, slots, g, z, r0, R * DP / 4, lds, [](int q, int &row, int &col) {
-    const int lane = q & 63, run = (q >> 6) % (DP / 8);
-    row = (q >> 6) / (DP / 8) * 32 + (lane & 31);
-    col = run * 8 + (lane >> 5) * 4;
+    const int lane = q & 63, run = (q >> 6) % (NO * 2);
+    row = (q >> 6) / (NO * 2) * 32 + (run & 1) * 16 + (lane & 15);
+    col = (run >> 1) * 16 + (lane >> 4) * 4;
   });
 }

@@ -234,7 +234,6 @@ struct AttendArgs {
   X(attend_f16_rows256, AttendArgs)     \
   X(attend_f16_wide64, AttendArgs)      \
   X(attend_f16_wide128, AttendArgs)     \
-  X(attend_f16_huge128, AttendArgs)     \
   X(attend_f16_any64, AttendArgs)       \
   X(attend_f16_any128, AttendArgs)      \
   X(attend_f16_any256, AttendArgs)      \
@@ -350,7 +349,7 @@ constexpr int kGatedAnyRows = 64, kGatedAnyCols = 32;      // tile of the gated 
 constexpr int kAttendRows = 16;       // query rows per workgroup
 constexpr int kAttendMaxWidth = 256;
 // Workgroups that share the keys of a tile: the join keeps a factor for each of its rows in workgroup memory
-// (rows kernels: at most 256 x 16 of 32 KB, wide ones 32 x 128 or 32 x 256).
+// (rows kernels: at most 256 x 16, wide ones 32 x 128, 16 KB each).
 constexpr int64_t kAttendMaxSplits = 256, kAttendMaxWideSplits = 32;
 constexpr int64_t kAttendMaxScratch = (int64_t)1 << 30;
 constexpr int kGapShare = 1;          // global average: log2 of the threads that share a pixel (vector form)

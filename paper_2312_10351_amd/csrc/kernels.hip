@@ -1682,7 +1682,6 @@ KATTEND(f32, float, 256)
 #undef KATTEND
 KDEF2(attend_f16_wide64, 256, 2, lds_attend_wide(64), AttendArgs, (attend_wide_body<64, 4>(a, b, lds)))
 KDEF2(attend_f16_wide128, 256, 2, lds_attend_wide(128), AttendArgs, (attend_wide_body<128, 4>(a, b, lds)))
-KDEF2(attend_f16_huge128, 512, 2, lds_attend_wide(128), AttendArgs, (attend_wide_body<128, 8>(a, b, lds)))
 
 // The 256-thread bodies by the vector registers they need (see the group kernels below):
 // X(kernel name, argument record, body call); T / tn: element type, C: access policy.

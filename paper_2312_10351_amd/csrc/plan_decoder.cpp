@@ -228,20 +228,17 @@ int attend_shape(const opara_op_desc &op, const opara_op_more &q, AttendShape *s
 // (`join`) and of every workgroup that is joined (`each`); records pass through memory at 2.5 TB/s.  Fitted to
 // 700 launches per type (1..2048 rows of 1..32 key heads, 128..65536 keys, 1..256 splits); the form and split it
 // picks are 2 % slower than the best in the mean.
-struct AttendForm { int kernel, any, rows, threads, key_tile; double alone, busy, fixed, join, each; };   // any: for unaligned keys, -1 none
-const AttendForm kAttendF16[3][3] = {
-    {{K_attend_f16_rows64, K_attend_f16_any64, 16, 256, 128, 7.3, 6.3, 3.1, 5.5, 0.10},
-     {K_attend_f16_wide64, -1, 128, 256, 64, 16.9, 11.7, 3.4, 2.4, 0.63},
-     {-1, -1, 0, 0, 0, 0, 0, 0, 0, 0}},
-    {{K_attend_f16_rows128, K_attend_f16_any128, 16, 256, 128, 8.3, 11.5, 4.2, 5.0, 0.25},
-     {K_attend_f16_wide128, -1, 128, 256, 64, 26.9, 21.1, 4.3, 3.5, 0.90},
-     {K_attend_f16_huge128, -1, 256, 512, 64, 32.5, 40.0, 5.6, 3.7, 1.08}},
-    {{K_attend_f16_rows256, K_attend_f16_any256, 16, 256, 128, 16.0, 22.0, 6.0, 5.0, 0.27},
-     {-1, -1, 0, 0, 0, 0, 0, 0, 0, 0},
-     {-1, -1, 0, 0, 0, 0, 0, 0, 0, 0}}};
-const AttendForm kAttendF32[3] = {{K_attend_f32_rows64, K_attend_f32_any64, 16, 256, 64, 18.4, 17.9, 3.1, 5.8, 0.085},
-                                  {K_attend_f32_rows128, K_attend_f32_any128, 16, 256, 64, 28.9, 34.7, 4.2, 5.7, 0.21},
-                                  {K_attend_f32_rows256, K_attend_f32_any256, 16, 256, 64, 54.1, 80.0, 6.6, 5.0, 0.27}};
+struct AttendForm { int kernel, any, rows, key_tile; double alone, busy, fixed, join, each; };   // any: for unaligned keys, -1 none
+const AttendForm kAttendF16[3][2] = {
+    {{K_attend_f16_rows64, K_attend_f16_any64, 16, 128, 7.3, 6.3, 3.1, 5.5, 0.10},
+     {K_attend_f16_wide64, -1, 128, 64, 16.9, 11.7, 3.4, 2.4, 0.63}},
+    {{K_attend_f16_rows128, K_attend_f16_any128, 16, 128, 8.3, 11.5, 4.2, 5.0, 0.25},
+     {K_attend_f16_wide128, -1, 128, 64, 26.9, 21.1, 4.3, 3.5, 0.90}},
+    {{K_attend_f16_rows256, K_attend_f16_any256, 16, 128, 16.0, 22.0, 6.0, 5.0, 0.27},
+     {-1, -1, 0, 0, 0, 0, 0, 0, 0}}};
+const AttendForm kAttendF32[3] = {{K_attend_f32_rows64, K_attend_f32_any64, 16, 64, 18.4, 17.9, 3.1, 5.8, 0.085},
+                                  {K_attend_f32_rows128, K_attend_f32_any128, 16, 64, 28.9, 34.7, 4.2, 5.7, 0.21},
+                                  {K_attend_f32_rows256, K_attend_f32_any256, 16, 64, 54.1, 80.0, 6.6, 5.0, 0.27}};
 
 struct AttendPick { const AttendForm *form; int64_t tiles, splits, counter_bytes, scratch; };
 
@@ -252,7 +249,7 @@ AttendPick attend_pick(const opara_op_desc &op, const AttendShape &s, bool vec, 
   const AttendForm *forms = f16 ? kAttendF16[size] : &kAttendF32[size];
   AttendPick best{};
   double least = 0.0;
-  for (int i = 0; i < (f16 ? 3 : 1); ++i) {
+  for (int i = 0; i < (f16 ? 2 : 1); ++i) {
     const AttendForm &f = forms[i];
     if (f.kernel < 0 || (!vec && f.any < 0) || (f.rows > kAttendRows && !(op.params.alpha > 0.f))) continue;
     const int64_t tiles = cdiv((int64_t)op.params.m * s.share, f.rows), work = tiles * s.kv_heads * s.batch;
@@ -311,7 +308,7 @@ int plan_attention(const opara_op_desc &op, const opara_op_more &q, const void *
   out->kernel = vec ? pick.form->kernel : pick.form->any;
   const int64_t gx = pick.tiles * pick.splits;
   if (gx * s.kv_heads * s.batch > kInt) return too_large("more rows than one launch holds", op);
-  out->gx = (uint32_t)gx; out->gy = (uint32_t)s.kv_heads; out->gz = (uint32_t)s.batch; out->block = (uint32_t)pick.form->threads;
+  out->gx = (uint32_t)gx; out->gy = (uint32_t)s.kv_heads; out->gz = (uint32_t)s.batch; out->block = 256;
   out->args.attend = a;
   return OPARA_OK;
 }
