@@ -87,62 +87,73 @@ __device__ __forceinline__ void attend_join(const AR &a, int64_t tile_id, const 
   if (!*last) return;
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   __syncthreads();                                           // `last` lies where the factors go
-  // ---- what every record counts for in a row: LR lanes share the row's records, eight loads in flight
+  // ---- what every record counts for in a row: LR lanes share the row's records, eight of each lane are requested at
+  // once, and with them, where there are few runs of four results, the first eight that a thread adds up
   constexpr int LR = NT / R;
   static_assert(LR >= 1 && LR <= 64 && (LR & (LR - 1)) == 0, "lanes per row");
   float *factor = (float *)lds;                              // [S][R]
+  const bool few = runs <= NT;
+  const int parts = runs * 8 <= NT ? 8 : runs * 4 <= NT ? 4 : runs * 2 <= NT ? 2 : 1;      // threads that share a run
+  const int q = t % (NT / parts), part = t / (NT / parts);
+  const float *from = slots + (int64_t)min(q, runs - 1) * 4;
+  floatx4 x[8];
   {
-    const int row = t / LR, part = t % LR;
+    const int row = t / LR, lane = t % LR;
     const float *stat = slots + R * DP + min(row, rows - 1);
-    auto each = [&](auto f) {
-      for (int s0 = part; s0 < S; s0 += 8 * LR) {
-        float m[8], e[8];
+    float m[8], e[8];
+    auto request = [&](int s0) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float *at = stat + (int64_t)min(s0 + i * LR, S - 1) * REC;
-          m[i] = at[0];
-          e[i] = at[R];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (s0 + i * LR < S) f(s0 + i * LR, m[i], e[i]);
+      for (int i = 0; i < 8; ++i) {
+        const float *at = stat + (int64_t)min(s0 + i * LR, S - 1) * REC;
+        m[i] = at[0];
+        e[i] = at[R];
       }
     };
+    request(lane);
+    if (few)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = *(const floatx4 *)(from + (int64_t)min(part + i * parts, S - 1) * REC);
     float most = -INFINITY, total = 0.f;
-    each([&](int, float m, float) { most = fmaxf(most, m); });
+    for (int s0 = lane; s0 < S; s0 += 8 * LR) {
+      if (s0 != lane) request(s0);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) most = fmaxf(most, m[i]);  // records past the last repeat it
+    }
 #pragma unroll
     for (int off = LR / 2; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, 64));
-    each([&](int s, float m, float e) {
-      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - most);
-      factor[s * R + row] = f;
-      total += f * e;
-    });
+    for (int s0 = lane; s0 < S; s0 += 8 * LR) {
+      if (S > 8 * LR) request(s0);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (s0 + i * LR >= S) break;
+        const float f = m[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[i] - most);
+        factor[(s0 + i * LR) * R + row] = f;
+        total += f * e[i];
+      }
+    }
 #pragma unroll
     for (int off = LR / 2; off > 0; off >>= 1) total += __shfl_xor(total, off, 64);
     const float inverse = attend_inverse(total);
-    for (int s = part; s < S; s += LR) factor[s * R + row] *= inverse;
+    for (int s = lane; s < S; s += LR) factor[s * R + row] *= inverse;
   }
   __syncthreads();
-  // ---- the sums.  Few runs of four results: `parts` threads share one; many: a thread takes eight at a time, so
-  // that as many loads are in flight.
-  if (runs <= NT) {
-    const int parts = runs * 8 <= NT ? 8 : runs * 4 <= NT ? 4 : runs * 2 <= NT ? 2 : 1, q = t % (NT / parts), part = t / (NT / parts);
+  // ---- the sums
+  if (few) {
     floatx4 *shared = (floatx4 *)(lds + (((size_t)R * S * 4 + 15) & ~(size_t)15));
     int row, col;
     place(min(q, runs - 1), row, col);
     const bool live = q < runs && row < rows && col < a.v_width;
+    row = min(row, rows - 1);
     floatx4 v = {0.f, 0.f, 0.f, 0.f};
-    if (live) {
-      const float *from = slots + (int64_t)q * 4;
-      int s = part;
-      for (; s + 7 * parts < S; s += 8 * parts) {
-        floatx4 x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = *(const floatx4 *)(from + (int64_t)(s + i * parts) * REC);
+    for (int i = 0; i < 8; ++i)
+      if (part + i * parts < S) v += x[i] * factor[(part + i * parts) * R + row];
+    for (int s0 = part + 8 * parts; s0 < S; s0 += 8 * parts) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v += x[i] * factor[(s + i * parts) * R + row];
-      }
-      for (; s < S; s += parts) v += *(const floatx4 *)(from + (int64_t)s * REC) * factor[s * R + row];
+      for (int i = 0; i < 8; ++i) x[i] = *(const floatx4 *)(from + (int64_t)min(s0 + i * parts, S - 1) * REC);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (s0 + i * parts < S) v += x[i] * factor[(s0 + i * parts) * R + row];
     }
     shared[t] = v;
     __syncthreads();
@@ -163,10 +174,9 @@ __device__ __forceinline__ void attend_join(const AR &a, int64_t tile_id, const 
       v[i] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
     for (int s = 0; s < S; ++s) {
-      const float *from = slots + (int64_t)s * REC;
-      floatx4 x[8];
+      const float *record = slots + (int64_t)s * REC;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = *(const floatx4 *)(from + (int64_t)min(q0 + i * NT, runs - 1) * 4);
+      for (int i = 0; i < 8; ++i) x[i] = *(const floatx4 *)(record + (int64_t)min(q0 + i * NT, runs - 1) * 4);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] += x[i] * factor[s * R + row[i]];
     }
@@ -278,12 +288,22 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
       const unsigned char *K = ring;
 #pragma unroll
       for (int i = 0; i < NQ; ++i) {
-        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+        floatx4 acc = {0.f, 0.f, 0.f, 0.f}, more[3];           // fp32: four chains, so that no instruction waits for the one before
+#pragma unroll
+        for (int e = 0; e < 3; ++e) more[e] = acc;
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
           const int row = i * 16 + r16;
-          acc = mma16<T>(*(const V *)(K + row * (DP * ES) + (((s * 4 + grp) ^ (row & 7)) * 16)), qf[s], acc);
+          const V kf = *(const V *)(K + row * (DP * ES) + (((s * 4 + grp) ^ (row & 7)) * 16));
+          if constexpr (ES == 2) {
+            acc = mma16<T>(kf, qf[s], acc);
+          } else {
+            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[0], qf[s][0], acc, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 3; ++e) more[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e + 1], qf[s][e + 1], more[e], 0, 0, 0);
+          }
         }
+        if constexpr (ES == 4) acc += (more[0] + more[1]) + more[2];
 #pragma unroll
         for (int e = 0; e < 4; ++e) p[i][e] = kt * KT + i * 16 + grp * 4 + e < mine ? acc[e] * a.scale : -INFINITY;
       }

@@ -418,12 +418,14 @@ class Session:
         import torch
         if self._index is None:
             self._index = torch.device(self.device).index or 0
-        handle = (torch.cuda.current_stream(self._index) if stream is None else stream).cuda_stream
-        if torch.cuda.current_device() == self._index:     # switching devices costs half as much as a launch
-            B.opara_run_eager(self.dag, handle)
+            self._eager = B.load().opara_run_eager
+        # The raw handle of the current stream: the stream object around it costs half as much as a launch.
+        handle = torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream.cuda_stream
+        if torch.cuda.current_device() == self._index:
+            B._check(self._eager(self.dag, handle))
         else:
             with torch.cuda.device(self._index):
-                B.opara_run_eager(self.dag, handle)
+                B._check(self._eager(self.dag, handle))
 
     def clear_outputs(self):
         for t in self.out_dev + list(self.out2_dev.values()):
