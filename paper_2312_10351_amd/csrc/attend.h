@@ -18,6 +18,40 @@
 constexpr int attend_ring_bytes(int dp) { return 2 * 64 * dp; }      // of one wavefront: a tile of keys, one of values
 constexpr int lds_attend_rows(int dp) { return 4 * attend_ring_bytes(dp); }
 
+constexpr float kAttendSlack = 8.f;
+
+// L loads of a wavefront bring its share of a tile of KT keys (or values) straight into workgroup memory.  A row's chunk
+// c lies in slot c ^ (row & 7): fragment reads of adjacent rows then differ in their banks.  Offsets inside a
+// tile are worked out once; a tile is a buffer that begins at its first row and ends with the last key, so
+// rows behind that arrive as zeros, and a step costs no vector instruction but the loads.
+template <typename T, int DP, int KT, int L> struct KeyStager {
+  static constexpr int ES = (int)sizeof(T), CH = DP * ES / 16, RL = 64 / CH;     // chunks per row, rows per load
+  uint32_t off[L], row_bytes;
+  const unsigned char *at;
+  int64_t step_bytes;
+  // share: this wavefront's number among those that fill the tile; the tile after next lies `tiles` further on.
+  __device__ __forceinline__ void init(const T *base, int64_t pitch, int width, int share, int first_tile, int tiles, int lane) {
+#pragma unroll
+    for (int l = 0; l < L; ++l) {
+      const int row = (share * L + l) * RL + lane / CH, d = ((lane % CH) ^ (row & 7)) * (16 / ES);
+      off[l] = d < width ? ((uint32_t)row * (uint32_t)pitch + (uint32_t)d) * ES : kOperandMaxBytes;
+    }
+    row_bytes = (uint32_t)pitch * ES;
+    at = (const unsigned char *)(base + (int64_t)first_tile * KT * pitch);
+    step_bytes = (int64_t)tiles * KT * pitch * ES;
+  }
+  // left: keys from the tile's first on
+  __device__ __forceinline__ void issue(int left, uint32_t lds) {
+    const i32x4 buf = buffer_of(at, (uint32_t)__builtin_amdgcn_readfirstlane(min(max(left, 0), KT)) * row_bytes);
+    // The clamp is a vector instruction: five wait states from there to the loads, which take the descriptor from
+    // scalar registers inside assembly that the compiler does not look into.
+    asm volatile("s_nop 4" : : "s"(buf));
+#pragma unroll
+    for (int l = 0; l < L; ++l) lds_load16(buf, off[l], 0, lds + l * 1024);
+    at += step_bytes;
+  }
+};
+
 // Over the four lanes that hold a query row: i, i ^ 16, i ^ 32, i ^ 48.  Lane swaps stay in the vector unit; a
 // shuffle goes through workgroup memory's crossbar.
 template <typename F> __device__ __forceinline__ float over_row(float v, F join) {
@@ -36,10 +70,10 @@ template <typename AR> struct AttendSight {
   int64_t ahead;                           // query row i of the sequence sees keys j < i + ahead
   bool causal;
   __device__ __forceinline__ AttendSight(const AR &a, int z, int last_row) {
-    length = a.lengths ? min(max(a.lengths[z], 0), a.n) : a.n;
+    length = __builtin_amdgcn_readfirstlane(a.lengths ? min(max(a.lengths[z], 0), a.n) : a.n);
     causal = a.causal != 0;
     ahead = a.causal == 2 ? (int64_t)length - a.m + 1 : (int64_t)a.first + 1;
-    end = limit(last_row);
+    end = __builtin_amdgcn_readfirstlane(limit(last_row));   // in a scalar register: loads take what follows from it at once
   }
   __device__ __forceinline__ int limit(int i) const {      // i: query row of the sequence
     return causal ? (int)max((int64_t)0, min((int64_t)length, i + ahead)) : length;
@@ -208,6 +242,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
   const int r = r0 + r16, qi = (int)fast_div((uint32_t)r, (uint32_t)a.share, a.div_share), head = g * a.share + r - qi * a.share;
   const AttendSight<AR> sight(a, z, (int)fast_div((uint32_t)min(rows - 1, r0 + 15), (uint32_t)a.share, a.div_share));
   const int mine = r < rows ? sight.limit(qi) : 0;          // this lane's query row sees keys [0, mine)
+  const int every = sight.limit((int)fast_div((uint32_t)r0, (uint32_t)a.share, a.div_share));      // every row sees these
   const int tiles = (sight.end + KT - 1) / KT;
   // Tiles go round the wavefronts of all workgroups that share them: what is read at a time lies together
   // (65536 keys of 8 heads beside each other, 32 splits: 53.2 us; in runs of tiles 61.1).
@@ -227,45 +262,34 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
           for (int e = 0; e < VE; ++e)
             if (d + e < a.width) v[e] = q[d + e];
       }
-      qf[s] = v;
+      qf[s] = a.negative ? -v : v;
     }
   }
   const T *kbase = (const T *)a.k + z * a.k_s[0] + g * a.k_s[2], *vbase = (const T *)a.v + z * a.v_s[0] + g * a.v_s[2];
   unsigned char *ring = lds + wave * RING;                  // a tile of keys, a tile of values
-  // A row's chunk c lies in slot c ^ (row & 7): fragment reads of adjacent rows then differ in their banks.
-  const int lrow = lane / CH, lslot = lane % CH;            // row and slot this lane fills (row + l * 64 / CH)
-  constexpr int RL = 64 / CH;                               // rows per load
-  static_assert(CH <= 64, "a row fits one load");
-
-  auto stage = [&](const T *base, int64_t pitch, int width, int kt, unsigned char *to) {
-    if constexpr (VEC) {
-      const i32x4 buf = buffer_of(base + (int64_t)kt * KT * pitch, kOperandMaxBytes);
+  typedef KeyStager<T, DP, KT, L> Stage;
+  Stage keys, values;
+  if constexpr (VEC) {
+    keys.init(kbase, a.k_s[1], a.width, 0, first, step, lane);
+    values.init(vbase, a.v_s[1], a.v_width, 0, first, step, lane);
+  }
+  // Rows at any address and distance: through registers.
+  auto copy = [&](const T *base, int64_t pitch, int width, int kt, unsigned char *to) {
 #pragma unroll
-      for (int l = 0; l < L; ++l) {
-        const int row = l * RL + lrow, chunk = lslot ^ (row & 7);
-        const bool in = kt * KT + row < sight.end && chunk * VE < width;
-        lds_load16(buf, in ? ((uint32_t)row * (uint32_t)pitch + (uint32_t)chunk * VE) * ES : kOperandMaxBytes, 0,
-                   lds_address(to) + l * 1024);
+    for (int l = 0; l < L; ++l) {
+      const int row = l * Stage::RL + lane / CH, key = kt * KT + row, d = ((lane % CH) ^ (row & 7)) * VE;
+      V v = {};
+      if (key < sight.end) {
+        const T *src = base + (int64_t)key * pitch + d;
+        if (d + VE <= width) v = *(const VU *)src;
+        else
+#pragma unroll
+          for (int e = 0; e < VE; ++e)
+            if (d + e < width) v[e] = src[e];
       }
-    } else {
-#pragma unroll
-      for (int l = 0; l < L; ++l) {
-        const int row = l * RL + lrow, chunk = lslot ^ (row & 7), key = kt * KT + row, d = chunk * VE;
-        V v = {};
-        if (key < sight.end) {
-          const T *src = base + (int64_t)key * pitch + d;
-          if (d + VE <= width) v = *(const VU *)src;
-          else
-#pragma unroll
-            for (int e = 0; e < VE; ++e)
-              if (d + e < width) v[e] = src[e];
-        }
-        *(V *)(to + l * 1024 + lane * 16) = v;
-      }
+      *(V *)(to + l * 1024 + lane * 16) = v;
     }
   };
-  auto stage_k = [&](int kt) { stage(kbase, a.k_s[1], a.width, kt, ring); };
-  auto stage_v = [&](int kt) { stage(vbase, a.v_s[1], a.v_width, kt, ring + TILE); };
 
   floatx4 o[NO];
 #pragma unroll
@@ -276,14 +300,18 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
   // the other's operand is on its way.  (Two slots each hold half the workgroups per CU and measured the same.)  Tiles past
   // the last load nothing (zeros), so that the number of loads in flight never varies.
   if constexpr (VEC) {
-    if (kt < tiles) { stage_k(kt); stage_v(kt); }
+    if (kt < tiles) {
+      keys.issue(sight.end - kt * KT, lds_address(ring));
+      values.issue(sight.end - kt * KT, lds_address(ring) + TILE);
+    }
   }
 #pragma nounroll
   for (; kt < tiles; kt += step) {
+    const int left = sight.end - (kt + step) * KT;          // of the tile after this one
     if constexpr (VEC) wait_loads<L>();
-    else stage_k(kt);
+    else copy(kbase, a.k_s[1], a.width, kt, ring);
     // ---- scores of KT keys
-    float p[NQ][4];
+    floatx4 p[NQ];
     {
       const unsigned char *K = ring;
 #pragma unroll
@@ -304,39 +332,45 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
           }
         }
         if constexpr (ES == 4) acc += (more[0] + more[1]) + more[2];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) p[i][e] = kt * KT + i * 16 + grp * 4 + e < mine ? acc[e] * a.scale : -INFINITY;
+        p[i] = acc;
       }
     }
     if constexpr (VEC) {
       asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the slot has been read: it may be refilled
-      stage_k(kt + step);
+      keys.issue(left, lds_address(ring));
     }
     // ---- running maximum and sum
-    float most = top;
+    if (kt * KT + KT > every)                                 // not for everybody
+#pragma unroll
+      for (int i = 0; i < NQ; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[i][e] = kt * KT + i * 16 + grp * 4 + e < mine ? p[i][e] : -INFINITY;
+    float most = -INFINITY;
 #pragma unroll
     for (int i = 0; i < NQ; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) most = fmaxf(most, p[i][e]);
-    most = row_max(most);
-    const float from = most == -INFINITY ? 0.f : most;      // a row that has seen nothing yet
-    const float shrink = __builtin_amdgcn_exp2f(top - from);
-    top = most;
-    sum *= shrink;
+    most = row_max(most) * a.scale;                         // a positive factor
+    if (__any(most > top + kAttendSlack)) {
+      const float now = fmaxf(most, top), shrink = __builtin_amdgcn_exp2f(top - (now == -INFINITY ? 0.f : now));
+      top = now;
+      sum *= shrink;
+#pragma unroll
+      for (int j = 0; j < NO; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[j][e] *= shrink;
+    }
+    const float from = top == -INFINITY ? 0.f : top;        // a row that has seen nothing yet
 #pragma unroll
     for (int i = 0; i < NQ; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        p[i][e] = __builtin_amdgcn_exp2f(p[i][e] - from);
+        p[i][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i][e], a.scale, -from));
         sum += p[i][e];
       }
-#pragma unroll
-    for (int j = 0; j < NO; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[j][e] *= shrink;
     // ---- O^T += V^T P^T; key e of a lane's step: 16 * (e / 4) + 4 * grp + e % 4
     if constexpr (VEC) wait_loads<L>();
-    else stage_v(kt);
+    else copy(vbase, a.v_s[1], a.v_width, kt, ring + TILE);
     const unsigned char *W = ring + TILE;
     V pf;
 #pragma unroll
@@ -366,7 +400,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
     }
     if constexpr (VEC) {
       asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-      stage_v(kt + step);
+      values.issue(left, lds_address(ring) + TILE);
     }
   }
 
@@ -432,7 +466,6 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
 // then probabilities may exceed one, by at most that, which their rounding, relative to each, does not see.
 // Measured, fp16, 32 heads over 8 of 128, 8192 rows (us): causal 573 (960 TFLOP/s), all keys 1094 (1005; without the
 // softmax 1050, a large matrix product reaches 1350); 16 heads of 64, 4096 rows 93 (738).
-constexpr float kAttendSlack = 8.f;
 constexpr int lds_attend_wide(int dp) { return 4 * 64 * dp * 2; }
 
 template <int DP, int NW, typename AR>
@@ -440,8 +473,8 @@ __device__ __forceinline__ void attend_wide_body(const AR &a, const Blk &b, unsi
   typedef half_t T;
   typedef half8 V;
   typedef V VU __attribute__((aligned(2)));
-  constexpr int KT = 64, CH = DP / 8, TILE = KT * DP * 2;     // keys per tile, 16-byte chunks per row, bytes
-  constexpr int L = TILE / 1024 / NW, RL = 64 / CH;           // loads of a wavefront per tile, rows per load
+  constexpr int KT = 64, TILE = KT * DP * 2;                  // keys per tile, bytes
+  constexpr int L = TILE / 1024 / NW;                         // loads of a wavefront per tile
   constexpr int NS = DP / 32, NO = DP / 16;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int grp = lane >> 4, r16 = lane & 15;
@@ -484,34 +517,23 @@ __device__ __forceinline__ void attend_wide_body(const AR &a, const Blk &b, unsi
           for (int e = 0; e < 8; ++e)
             if (d + e < a.width) v[e] = q[d + e];
       }
-      qf[x][s] = v;
+      qf[x][s] = a.negative ? -v : v;
     }
   }
-  const T *kbase = (const T *)a.k + z * a.k_s[0] + g * a.k_s[2], *vbase = (const T *)a.v + z * a.v_s[0] + g * a.v_s[2];
-  const int lrow = lane / CH, lslot = lane % CH;
-  auto stage = [&](const T *base, int64_t pitch, int width, int kt, unsigned char *to) {
-    const i32x4 buf = buffer_of(base + (int64_t)kt * KT * pitch, kOperandMaxBytes);
-#pragma unroll
-    for (int l = 0; l < L; ++l) {
-      const int row = (wave * L + l) * RL + lrow, chunk = lslot ^ (row & 7);
-      const bool in = kt * KT + row < sight.end && chunk * 8 < width;
-      lds_load16(buf, in ? ((uint32_t)row * (uint32_t)pitch + (uint32_t)chunk * 8) * 2u : kOperandMaxBytes, 0,
-                 lds_address(to) + (wave * L + l) * 1024);
-    }
-  };
-  auto issue = [&](int kt, int slot) {
-    stage(kbase, a.k_s[1], a.width, kt, lds + slot * TILE);
-    stage(vbase, a.v_s[1], a.v_width, kt, lds + (2 + slot) * TILE);
-  };
-
+  KeyStager<T, DP, KT, L> keys, values;
+  keys.init((const T *)a.k + z * a.k_s[0] + g * a.k_s[2], a.k_s[1], a.width, wave, split, a.splits, lane);
+  values.init((const T *)a.v + z * a.v_s[0] + g * a.v_s[2], a.v_s[1], a.v_width, wave, split, a.splits, lane);
+  const uint32_t base = lds_address(lds) + wave * L * 1024;
   floatx4 o[NO][2];
 #pragma unroll
   for (int j = 0; j < NO; ++j)
 #pragma unroll
     for (int x = 0; x < 2; ++x) o[j][x] = floatx4{0.f, 0.f, 0.f, 0.f};
   float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
-  auto issue_k = [&](int kt, int slot) { stage(kbase, a.k_s[1], a.width, kt, lds + slot * TILE); };
-  auto issue_v = [&](int kt, int slot) { stage(vbase, a.v_s[1], a.v_width, kt, lds + (2 + slot) * TILE); };
+  auto issue = [&](int kt, int slot) {                        // in increasing order
+    keys.issue(sight.end - kt * KT, base + slot * TILE);
+    values.issue(sight.end - kt * KT, base + (2 + slot) * TILE);
+  };
   auto scores = [&](floatx4 (&s)[4][2], int slot) {
     const unsigned char *K = lds + slot * TILE;
 #pragma unroll
@@ -587,13 +609,13 @@ __device__ __forceinline__ void attend_wide_body(const AR &a, const Blk &b, unsi
       }
   };
 
-  if (split < tiles) { issue_k(split, 0); issue_v(split, 0); }
+  if (split < tiles) issue(split, 0);
   int slot = 0;
   auto turn = [&](int kt, auto masked_tag) {
     wait_loads_and_meet<0>();
     const int at = slot;
     slot ^= 1;
-    if (kt + a.splits < tiles) { issue_k(kt + a.splits, slot); issue_v(kt + a.splits, slot); }
+    if (kt + a.splits < tiles) issue(kt + a.splits, slot);
     if (decltype(masked_tag)::value && kt * KT >= reach) return;
     floatx4 s[4][2];
     __builtin_amdgcn_s_setprio(1);

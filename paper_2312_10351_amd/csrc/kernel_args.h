@@ -127,7 +127,8 @@ struct AttendArgs {
   int32_t batch, causal, first; // causal: 0 no, 1 from `first`, 2 to the sequence's end
   int32_t tiles, splits;
   uint32_t div_share, div_splits;
-  float scale;                  // alpha * log2(e): exponentials are powers of two
+  float scale;                  // |alpha| * log2(e), above zero: exponentials are powers of two
+  int32_t negative;             // alpha < 0: the queries change sign
 };
 
 // X(name, ArgsType).  Order defines kernel ids.

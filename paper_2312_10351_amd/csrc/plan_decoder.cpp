@@ -1,6 +1,7 @@
 // Launch planning of a decoder's blocks: rotary positions, the norms around a residual sum, the gated
 // half of a feed-forward block, attention (host only, no HIP calls).
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include "opara_internal.h"
@@ -251,7 +252,7 @@ AttendPick attend_pick(const opara_op_desc &op, const AttendShape &s, bool vec, 
   double least = 0.0;
   for (int i = 0; i < (f16 ? 2 : 1); ++i) {
     const AttendForm &f = forms[i];
-    if (f.kernel < 0 || (!vec && f.any < 0) || (f.rows > kAttendRows && !(op.params.alpha > 0.f))) continue;
+    if (f.kernel < 0 || (!vec && f.any < 0)) continue;
     const int64_t tiles = cdiv((int64_t)op.params.m * s.share, f.rows), work = tiles * s.kv_heads * s.batch;
     for (int64_t n = 1; n <= kAttendMaxSplits; n = n < 4 ? n + 1 : n + n / 2) {
       if (n > 1 && n * f.key_tile > s.keys) break;           // two tiles for every wavefront
@@ -285,10 +286,11 @@ int plan_attention(const opara_op_desc &op, const opara_op_more &q, const void *
   std::memcpy(a.k_s, s.strides[1], sizeof a.k_s);
   std::memcpy(a.v_s, s.strides[2], sizeof a.v_s);
   std::memcpy(a.y_s, s.strides[3], sizeof a.y_s);
-  // Loads straight into workgroup memory need aligned 16-byte pieces, and 32-bit offsets inside a tile of keys.
+  // Loads straight into workgroup memory need aligned 16-byte pieces, rows that do not overlap (a tile of keys
+  // ends with its last row) and 32-bit offsets inside a tile.
   auto vectors = [&](const void *base, const int64_t *st, int64_t width) {
     return aligned16(base) && width % ve == 0 && st[0] % ve == 0 && st[1] % ve == 0 && st[2] % ve == 0 &&
-           st[1] < (int64_t)kOperandMaxBytes / (64 * 4);
+           st[1] >= width && st[1] < (int64_t)kOperandMaxBytes / (64 * 4);
   };
   const bool vec = vectors(a.k, a.k_s, q.width) && vectors(a.v, a.v_s, s.v_width);
   const AttendPick pick = attend_pick(op, s, vec, q.scratch ? q.scratch_bytes : 0);
@@ -296,7 +298,9 @@ int plan_attention(const opara_op_desc &op, const opara_op_more &q, const void *
   a.batch = (int32_t)s.batch;
   a.causal = (p.flags & OPARA_FLAG_CAUSAL) ? 1 : (p.flags & OPARA_FLAG_CAUSAL_END) ? 2 : 0;
   a.first = q.first;
-  a.scale = p.alpha * 1.44269504088896341f;
+  // Above zero, so that a masked score stays -inf: with alpha 0 all visible keys count the same.
+  a.scale = std::max(std::fabs(p.alpha) * 1.44269504088896341f, FLT_MIN);
+  a.negative = p.alpha < 0.f;
   a.tiles = (int32_t)pick.tiles;
   a.splits = (int32_t)pick.splits;
   if (a.splits > 1) {
