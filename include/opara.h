@@ -141,10 +141,9 @@ typedef struct {
  *                     Y[b][i][h] = softmax over the visible j of (alpha Q[b][i][h] . K[b][j][g]) . V[b][j][g].
  *                     inputs: Q, K, V and optionally int32[batch], the valid key rows of every sequence
  *                     (below 0 counts as 0, above n as n; without it n).  CAUSAL, CAUSAL_END: see
- *                     opara_flags.  A query row that sees no key gives zeros.  Key and value rows behind
- *                     a sequence's length, and those behind the last one that a query row of it sees,
- *                     are not used, whatever they hold; inside, a value row that some query rows see must be finite
- *                     for the others to be.  strides: elements between sequences, rows and heads of
+ *                     opara_flags.  A query row that sees no key gives zeros, and nothing of a key or value row that
+ *                     it does not see reaches it, whatever that row holds (NaN included).  alpha: any sign;
+ *                     with 0 all visible keys count alike.  strides: elements between sequences, rows and heads of
  *                     Q, K, V and Y; a triple of zeros = packed [batch][rows][heads][width].
  *                     scratch: see opara_scratch_bytes.
  * heads ... beta, strides, out2 and scratch are fields of opara_op_more.

@@ -97,6 +97,54 @@ __device__ __forceinline__ void attend_store(const AR &a, int g, int z, int r, i
 // One over a sum of probabilities; a row that has seen nothing gives zeros, NaN stays.
 __device__ __forceinline__ float attend_inverse(float sum) { return sum > 0.f ? 1.0f / sum : sum == 0.f ? 0.f : sum; }
 
+// A value row that one query row sees and another does not may hold infinities or NaN; a probability of zero does not
+// take them out of a product.  Where a tile has such keys its values are looked over first (once per tile of
+// query rows under a causal mask), and only if one is not finite, what is not is added to the rows that see
+// it and taken out of the tile.
+template <typename T, int BYTES> __device__ __forceinline__ bool any_not_finite(const unsigned char *tile, int lane) {
+  constexpr uint32_t VALUE = sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu, STEP = sizeof(T) == 2 ? 0x04000400u : 0x00800000u;
+  uint32_t found = 0;
+#pragma unroll 4
+  for (int l = 0; l < BYTES; l += 1024) {
+    const i32x4 w = *(const i32x4 *)(tile + l + lane * 16);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) found |= ((uint32_t)w[e] & VALUE) + STEP;      // an exponent of ones carries into the sign
+  }
+  return __any((found & ~VALUE) != 0);
+}
+// tile: KT values from key `first` on; a lane holds result columns j * 16 + grp * 4 .. + 3, at(j, x), of NX query
+// rows that see keys below limit(x).
+template <typename T, int DP, int KT, int NX, typename F, typename G>
+__device__ __forceinline__ void add_infinite(const unsigned char *tile, int first, int grp, F limit, G at) {
+  typedef typename Run4<T>::type R;
+  constexpr int ES = (int)sizeof(T);
+#pragma nounroll
+  for (int key = 0; key < KT; ++key)
+#pragma unroll
+    for (int j = 0; j < DP / 16; ++j) {
+      const int byte = (j * 16 + grp * 4) * ES;
+      const R v = *(const R *)(tile + key * (DP * ES) + (((byte >> 4) ^ (key & 7)) << 4) + (byte & 15));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float f = (float)v[e], add = fabsf(f) < INFINITY ? 0.f : f;
+#pragma unroll
+        for (int x = 0; x < NX; ++x) at(j, x)[e] += first + key < limit(x) ? add : 0.f;
+      }
+      __builtin_amdgcn_sched_barrier(0);                     // no registers for what hardly ever runs
+    }
+}
+template <typename T, int BYTES> __device__ __forceinline__ void drop_infinite(unsigned char *part, int lane) {
+  typedef typename Vec16<T>::type V;
+#pragma nounroll
+  for (int l = 0; l < BYTES; l += 1024) {
+    V v = *(const V *)(part + l + lane * 16);
+#pragma unroll
+    for (int e = 0; e < Vec16<T>::N; ++e) v[e] = fabsf((float)v[e]) < INFINITY ? v[e] : (T)0;
+    *(V *)(part + l + lane * 16) = v;
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+}
+
 // The workgroups that share a tile's keys meet.  Each has left a record of R maxima, R sums and R x DP results in
 // `slots` with agent-scope stores, which pass the caches that XCDs do not share; it is counted once its stores have
 // completed, and whoever counts last invalidates its caches and joins the records in their order.
@@ -375,29 +423,31 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
     V pf;
 #pragma unroll
     for (int e = 0; e < VE; ++e) pf[e] = (T)p[e / 4][e % 4];
-    if constexpr (ES == 2) {
-#pragma unroll
-      for (int j = 0; j < NO; ++j) {
+    auto value = [&](int j) {
+      if constexpr (ES == 2) {
         half4 v[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int row = h * 16 + grp * 4 + (r16 >> 2);
           v[h] = lds_read_transposed(W + row * (DP * ES) + (((j * 2 + ((r16 >> 1) & 1)) ^ (row & 7)) * 16) + (r16 & 1) * 8);
         }
-        o[j] = mma16<T>(__builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7), pf, o[j]);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < NO; ++j) {
+        return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+      } else {
         V v;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int row = grp * 4 + e;
           v[e] = *(const T *)(W + row * (DP * ES) + (((j * 4 + (r16 >> 2)) ^ (row & 7)) * 16) + (r16 & 3) * 4);
         }
-        o[j] = mma16<T>(v, pf, o[j]);
+        return v;
       }
+    };
+    if (every < sight.end && kt * KT + KT > every && any_not_finite<T, TILE>(W, lane)) {
+      add_infinite<T, DP, KT, 1>(W, kt * KT, grp, [&](int) { return mine; }, [&](int j, int) -> floatx4 & { return o[j]; });
+      drop_infinite<T, TILE>(ring + TILE, lane);
     }
+#pragma unroll
+    for (int j = 0; j < NO; ++j) o[j] = mma16<T>(value(j), pf, o[j]);
     if constexpr (VEC) {
       asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
       values.issue(left, lds_address(ring) + TILE);
@@ -591,22 +641,32 @@ __device__ __forceinline__ void attend_wide_body(const AR &a, const Blk &b, unsi
         }
     }
   };
+  auto value = [&](int slot, int q, int j) {
+    half4 v[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int row = q * 32 + h * 16 + grp * 4 + (r16 >> 2), chunk = j * 2 + ((r16 >> 1) & 1);
+      v[h] = lds_read_transposed(lds + (2 + slot) * TILE + row * (DP * 2) + ((chunk ^ (row & 7)) * 16) + (r16 & 1) * 8);
+    }
+    return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+  };
   auto context = [&](int slot) {
-    const unsigned char *W = lds + (2 + slot) * TILE;
 #pragma unroll
     for (int q = 0; q < 2; ++q)
 #pragma unroll
       for (int j = 0; j < NO; ++j) {
-        half4 v[2];
+        const V v = value(slot, q, j);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int row = q * 32 + h * 16 + grp * 4 + (r16 >> 2), chunk = j * 2 + ((r16 >> 1) & 1);
-          v[h] = lds_read_transposed(W + row * (DP * 2) + ((chunk ^ (row & 7)) * 16) + (r16 & 1) * 8);
-        }
-        const V vf = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-        for (int x = 0; x < 2; ++x) o[j][x] = mma16<T>(vf, p[q][x], o[j][x]);
+        for (int x = 0; x < 2; ++x) o[j][x] = mma16<T>(v, p[q][x], o[j][x]);
       }
+  };
+  // All wavefronts come here, and read the tile before any of them changes it.
+  auto take_infinite = [&](int slot, int kt) {
+    add_infinite<T, DP, KT, 2>(lds + (2 + slot) * TILE, kt * KT, grp, [&](int x) { return mine[x]; },
+                               [&](int j, int x) -> floatx4 & { return o[j][x]; });
+    __syncthreads();
+    drop_infinite<T, TILE / NW>(lds + (2 + slot) * TILE + wave * (TILE / NW), lane);
+    __syncthreads();
   };
 
   if (split < tiles) issue(split, 0);
@@ -616,12 +676,21 @@ __device__ __forceinline__ void attend_wide_body(const AR &a, const Blk &b, unsi
     const int at = slot;
     slot ^= 1;
     if (kt + a.splits < tiles) issue(kt + a.splits, slot);
-    if (decltype(masked_tag)::value && kt * KT >= reach) return;
+    bool apart = false;
+    if constexpr (decltype(masked_tag)::value) {
+      apart = a.causal && any_not_finite<T, TILE>(lds + (2 + at) * TILE, lane);
+      if (kt * KT >= reach) {
+        if (apart) take_infinite(at, kt);
+        return;
+      }
+    }
     floatx4 s[4][2];
     __builtin_amdgcn_s_setprio(1);
     scores(s, at);
     __builtin_amdgcn_s_setprio(0);
     soften(s, kt, masked_tag);
+    if constexpr (decltype(masked_tag)::value)
+      if (apart) take_infinite(at, kt);
     __builtin_amdgcn_s_setprio(1);
     context(at);
     __builtin_amdgcn_s_setprio(0);

@@ -68,6 +68,7 @@ int plan_norm(const opara_op_desc &op, const opara_op_more &q, const void *const
   if (!(p.eps >= 0.f)) return fail("negative eps", op);
   const bool after = p.flags & OPARA_FLAG_NORM_AFTER, before = p.flags & OPARA_FLAG_NORM_BEFORE;
   if (q.out2 && !before) return fail("a second result goes with a norm of the sum", op);
+  if (q.out2 && q.out2 == op.out) return fail("both results in one buffer", op);
   if ((op.weight || op.bias) && !after && !before) return fail("weights without a norm", op);
   NormArgs a;
   std::memset(&a, 0, sizeof a);

@@ -88,6 +88,7 @@ class Session:
                 chans = a.shape[-3] if a.ndim >= 3 and isinstance(a, np.ndarray) else 0
                 if chans and a.ndim >= 3 and chans % ve and all(o.type == "conv2d" for o in users.get(slot, [])):
                     self.ext_pad[slot] = (chans + ve - 1) // ve * ve
+        self._check_tensors()
         self.ext_dev = [self._upload(self._to_physical_input(a, self.ext_pad.get(i))) for i, a in enumerate(wl.ext_inputs)]
         self.out_dev = [None] * len(wl.ops)
         self.out2_dev = {}                  # second results
@@ -171,12 +172,46 @@ class Session:
         return int(np.prod(op.out_shape)) * (self.wl.batch if _is_image(op) else 1)
 
     # ---- device memory (PyTorch) or fake addresses when there is no device
+    def _check_tensors(self):
+        """Positions and lengths are int32; tensors that are used in place have the type and size that the operators read."""
+        import torch
+        wl = self.wl
+        own = {"f32": torch.float32, "f16": torch.float16}[wl.dtype]
+
+        def check(t, numel, dtype, what):
+            if isinstance(t, torch.Tensor) and (t.dtype != dtype or t.numel() < numel):
+                raise ValueError(f"{what}: {numel} elements of {dtype} are read, the tensor has {t.numel()} of {t.dtype}")
+
+        for op in wl.ops:
+            whole = {"rotary": 1, "attention": 3}.get(op.type)
+            for i, (u, shape) in enumerate(zip(op.inputs, op.in_shapes)):
+                if u >= 0:
+                    continue
+                t, what = wl.ext_inputs[-u - 1], f"input {i} of {op.name}"
+                if i == whole and str(t.dtype).split(".")[-1] != "int32":
+                    raise ValueError(f"{what}: positions and lengths are int32, not {t.dtype}")
+                check(t, int(np.prod(shape)) * (wl.batch if _is_image(op) else 1), torch.int32 if i == whole else own, what)
+            if op.id not in wl.weights:
+                continue
+            q, w = op.params, wl.weights[op.id]
+            cols = {"conv2d": "cout", "gemm": "n", "gated": "n"}.get(op.type)
+            if op.type == "residual_norm":
+                n_w = n_b = (q["after"] + q["before"]) * op.out_shape[1]
+            elif cols:
+                n_b = q[cols] * (2 if op.type == "gated" else 1)
+                n_w = n_b * (q["cin"] * q["kh"] * q["kw"] if op.type == "conv2d" else q["k"])
+            else:
+                continue
+            check(w["w"], n_w, own, f"weight of {op.name}")
+            check(w["b"], n_b, torch.float32, f"bias of {op.name}")
+
     def _upload(self, arr):
         if self.device is None:
             return self._fake_ptr(arr.nbytes)
         import torch
         if isinstance(arr, torch.Tensor):
-            if arr.device != torch.device(self.device) or not arr.is_contiguous():
+            on = torch.device(self.device)
+            if arr.device.type != on.type or (on.index is not None and arr.device.index != on.index) or not arr.is_contiguous():
                 raise ValueError(f"a device tensor of a workload must be contiguous and on {self.device}")
             return arr
         return torch.from_numpy(np.ascontiguousarray(arr)).to(self.device)

@@ -5,12 +5,13 @@ from fractions import Fraction
 
 import numpy as np
 import pytest
+import torch
 
 from decoder_util import ATTEND as ATTEND_SIZES, GATED as GATED_SIZES, NORM as NORM_SIZES, build, describe
 from oracle import executor, ops as O
 from paper_2312_10351_amd import binding as B
 from paper_2312_10351_amd.runtime import Session
-from workloads import Builder, Second, decoder_like
+from workloads import Builder, Second, Workload, decoder_like
 
 
 # ---- the oracle ---------------------------------------------------------------------------
@@ -114,6 +115,7 @@ ATTEND = dict(m=4, n=9, heads=4, kv_heads=2, width=8, alpha=1.0)
     (B.RESIDUAL_NORM, 2, NORM, dict(m=0)), (B.RESIDUAL_NORM, 2, NORM, dict(n=-1)), (B.RESIDUAL_NORM, 4, NORM, dict()),
     (B.RESIDUAL_NORM, 3, NORM, dict(batch=3)), (B.RESIDUAL_NORM, 2, NORM, dict(batch=2)), (B.RESIDUAL_NORM, 2, NORM, dict(eps=-1.0)),
     (B.RESIDUAL_NORM, 2, NORM, dict(eps=math.nan)), (B.RESIDUAL_NORM, 2, NORM, dict(flags=0, out2=0x900000)),
+    (B.RESIDUAL_NORM, 2, NORM, dict(out2=0x100000)),
     (B.RESIDUAL_NORM, 2, NORM, dict(flags=0, weight=0x2000)),
     (B.GATED, 1, GATED, dict(weight=None)), (B.GATED, 2, GATED, dict()), (B.GATED, 1, GATED, dict(activation=5)),
     (B.GATED, 1, GATED, dict(activation=-1)), (B.GATED, 1, GATED, dict(k=0)), (B.GATED, 1, GATED, dict(a_row_stride=7)),
@@ -218,6 +220,42 @@ def test_attention_sizes_of_the_gpu_tests_reach_every_form():
         assert set(taken) == {name for name in every if name.startswith(f"attend_{dtype}_")}
         for name in ("rows64", "rows128") + (("wide64", "wide128") if dtype == "f16" else ()):
             assert taken[f"attend_{dtype}_{name}"] == {False, True}, name
+
+
+@pytest.mark.parametrize("width, v_width, strides, kernel", [
+    (64, 64, [0, 0, 0], "rows"), (64, 64, [0, 64, 64], "rows"), (64, 64, [0, 8, 0], "any"), (64, 64, [0, 132, 64], "any"), (60, 64, [0, 128, 64], "any"),
+    (64, 60, [0, 128, 64], "any"), (64, 56, [0, 128, 64], "rows"), (64, 64, [0, 1 << 24, 64], "any"), (64, 64, [0, 0, 64], "any")])
+def test_attention_loads_only_rows_that_it_can_through_buffers(width, v_width, strides, kernel):
+    """Unaligned, overlapping and far keys take the form that reads them through registers."""
+    packed = strides == [0, 0, 0]
+    op = describe(B.ATTENTION, "f16", 3, m=1, n=500, heads=2, kv_heads=2, width=width, v_width=v_width, alpha=1.0,
+                  strides=[[0] * 3, strides, [0, 128, 64], [0] * 3])
+    assert build(op) == [f"attend_f16_{kernel}64"], packed
+
+
+# ---- tensors of a workload ------------------------------------------------------------------
+
+def tensors(**changed):
+    """An attention of a batch of two and the gated block and norm after it, over torch tensors (not on a device: host only)."""
+    t = dict(q=torch.zeros(6, 32, dtype=torch.float16), k=torch.zeros(10, 32, dtype=torch.float16), lengths=torch.zeros(2, dtype=torch.int32),
+             w=torch.zeros(48, 32, dtype=torch.float16), b=torch.zeros(48), g=torch.zeros(1, 24, dtype=torch.float16), nb=torch.zeros(1, 24))
+    t.update(changed)
+    b = Builder("tensors", "f16")
+    e = [b.ext(s) for s in ((6, 32), (10, 32), (2,))]
+    a = b.attention(e[0], e[1], e[1], heads=2, width=16, batch=2, lengths=e[2])
+    b.residual_norm(b.gated(a, 6, 32, 24))
+    return Workload("tensors", "f16", b.ops, [t["q"], t["k"], t["lengths"]], {1: {"w": t["w"], "b": t["b"]}, 2: {"w": t["g"], "b": t["nb"]}})
+
+
+def test_tensors_used_in_place_are_checked():
+    Session(tensors(), device=None)
+    Session(tensors(lengths=np.zeros(2, dtype=np.int32)), device=None)
+    for bad in (dict(q=torch.zeros(6, 32)), dict(k=torch.zeros(9, 32, dtype=torch.float16)), dict(lengths=torch.zeros(2, dtype=torch.int64)),
+                dict(lengths=torch.zeros(1, dtype=torch.int32)), dict(lengths=np.zeros(2, dtype=np.int64)), dict(w=torch.zeros(48, 32)),
+                dict(w=torch.zeros(47, 32, dtype=torch.float16)), dict(b=torch.zeros(48, dtype=torch.float16)), dict(b=torch.zeros(24)),
+                dict(g=torch.zeros(1, 23, dtype=torch.float16)), dict(nb=torch.zeros(1, 24, dtype=torch.float64))):
+        with pytest.raises(ValueError):
+            Session(tensors(**bad), device=None)
 
 
 # ---- in a DAG ------------------------------------------------------------------------------

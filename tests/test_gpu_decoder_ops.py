@@ -261,6 +261,79 @@ def test_attention_lengths_are_read_at_every_launch():
     s.close()
 
 
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("m, heads, kv, width, causal", [(20, 2, 1, 64, "start"), (1000, 8, 4, 128, "start"), (900, 8, 8, 64, "end"), (70, 2, 2, 37, "start"),
+                                                         (33, 1, 1, 256, "end"), (129, 3, 3, 130, "start")])
+def test_attention_of_rows_that_do_not_see_what_is_not_finite(dtype, m, heads, kv, width, causal):
+    """Under a causal mask later keys and values may hold anything: rows before them are as without them."""
+    first, second = m // 3, m * 2 // 3
+    g = gen(m)
+    q, k, v = (D.normal(g, (m, h * width), dtype) for h in (heads, kv, kv))
+    v[first, 0::4], v[first, 1::4], v[first, 2::4] = np.inf, -np.inf, np.nan
+    k[second:], v[second:] = np.nan, np.inf
+    kw = dict(heads=heads, width=width, kv_heads=kv, causal=causal)
+    s = D.bind(lambda b, e: b.attention(*e, **kw), [q, k, v], dtype=dtype)
+    got = run(s).result(0).clone()
+    s.close()
+    cut = lambda rows: [t.to(DEV) for t in (q[:rows], k[:rows], v[:rows].nan_to_num(0.0, 0.0, 0.0))]
+    head = dict(kw, causal="start")
+    D.within(got[:first], *D.attention(*cut(first), dtype, **head), dtype, "before")
+    want, bound = D.attention(*cut(second), dtype, **head)
+    c = torch.arange(heads * width, device=DEV)
+    column = (c // width // (heads // kv) * width + c % width) % 4        # of the values
+    D.within(got[first:second, column == 3], want[first:second, column == 3], bound[first:second, column == 3], dtype, "finite columns")
+    seen = got[first:second].float()
+    assert (seen[:, column == 0] == np.inf).all() and (seen[:, column == 1] == -np.inf).all() and seen[:, column == 2].isnan().all()
+    assert got[second:].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("m, n, width, causal", [(1, 3000, 64, None), (50, 700, 128, "end"), (1000, 500, 64, "start"), (9, 100, 33, None)])
+@pytest.mark.parametrize("alpha", [-0.4, 0.0])
+def test_attention_of_any_factor(dtype, m, n, width, causal, alpha):
+    g = gen(n)
+    q, k, v = (D.normal(g, (r, 4 * width), dtype) for r in (m, n, n))
+    kw = dict(heads=4, width=width, causal=causal, alpha=alpha)
+    s = D.bind(lambda b, e: b.attention(*e, **kw), [q, k, v], dtype=dtype)
+    D.within(run(s).result(0), *D.attention(*(t.to(DEV) for t in (q, k, v)), dtype, **kw), dtype)
+    s.close()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("pitch, scratch", [(8, True), (0, False)])
+def test_attention_over_windows_of_one_row(dtype, pitch, scratch):
+    """Keys and values that overlap, or are one row for all."""
+    n, width = 900, 64
+    g = gen(pitch)
+    row = D.normal(g, (n * 8 + width,), dtype)
+    q = D.normal(g, (2, width), dtype)
+    keys = row.as_strided((n, width), (pitch, 1)).contiguous()
+    y = torch.zeros(2, width, dtype=D.TORCH[dtype], device=DEV)
+    d = D.describe(B.ATTENTION, dtype, 3, m=2, n=n, heads=1, width=width, alpha=0.125, out=y.data_ptr(),
+                   strides=[[0] * 3, [0, pitch, 1], [0, pitch, 1], [0] * 3])
+    d[1].scratch_bytes = B.opara_scratch_bytes(*d) if scratch else 0
+    room = torch.zeros(max(256, d[1].scratch_bytes), dtype=torch.uint8, device=DEV)
+    d[1].scratch = room.data_ptr() if scratch else None
+    eager(d, [q.to(DEV), row.to(DEV), row.to(DEV)], dtype)
+    D.within(y, *D.attention(*(t.to(DEV) for t in (q, keys, keys)), dtype, width=width), dtype)
+
+
+def test_attention_with_less_scratch_than_asked_for():
+    q, k, v = (D.normal(gen(i), (r, 4 * 128), "f16") for i, r in enumerate((1, 20000, 20000)))
+    on = [t.to(DEV) for t in (q, k, v)]
+    want = D.attention(*on, "f16", heads=4, width=128)
+    d = D.describe(B.ATTENTION, "f16", 3, m=1, n=20000, heads=4, width=128, alpha=128 ** -0.5)
+    asked = B.opara_scratch_bytes(*d)
+    for given in (asked, asked // 2, asked // 7, 256, 0):
+        y = torch.zeros(1, 4 * 128, dtype=torch.float16, device=DEV)
+        room = torch.zeros(given + 256, dtype=torch.uint8, device=DEV)
+        room[given:] = 77
+        d[0].out, d[1].scratch, d[1].scratch_bytes = y.data_ptr(), room.data_ptr(), given
+        eager(d, on, "f16")
+        D.within(y, *want, "f16", str(given))
+        assert (room[given:] == 77).all()
+
+
 def test_attention_over_more_than_four_gigabytes_of_keys():
     """Rows far apart: offsets of the last keys pass 32 bits."""
     n, width, pitch = 2100, 64, 1 << 21
@@ -356,6 +429,50 @@ def test_persistent_and_chained_executors_refuse():
         with pytest.raises(B.OparaError) as e:
             capture()
         assert e.value.status == B.EUNSUPPORTED
+    s.close()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_launches_captured_into_the_callers_graph(dtype):
+    """A session's launches among a program's own operations, in a graph that is replayed between eager work."""
+    wl = decoder_like(dtype=dtype, layers=1, seq=3, states=900, hidden=256, heads=4, kv_heads=2, ffn=300, past=7)
+    s = Session(wl, device=DEV)
+    run(s)
+    x, last = torch.zeros_like(s.ext_dev[0]), len(wl.ops) - 1
+    x.copy_(s.ext_dev[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.ext_dev[0].copy_(x)
+        s.launch()
+        captured = s.result(last) * 2
+    for step in range(4):
+        x.mul_(0.5).add_(step)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = captured.clone()
+        s.clear_outputs()
+        assert torch.equal(run(s).result(last) * 2, got) and got.abs().max() > 0
+    s.close()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_attentions_beside_each_other(dtype):
+    """Independent ones of a wave run at once, each with its own scratch memory."""
+    b = Builder("beside", dtype)
+    k, v = b.ext((3000, 128)), b.ext((3000, 128))
+    for i in range(5):
+        b.attention(b.ext((1 + i, 256)), k, v, heads=4, width=64, kv_heads=2, causal="end" if i % 2 else None)
+    b.rowwise("add", [0, 0], 1, 256)
+    wl = b.build(4)
+    ref = executor.run_dag(wl)
+    s = Session(wl, device=DEV)
+    assert len({s.descs[i].out for i in range(5)}) == 5
+    for mode in (B.PARALLEL, B.FUSED, B.SEQUENTIAL):
+        exe = s.capture(mode)
+        for _ in range(3):
+            s.clear_outputs()
+            s.replay(exe)
+            assert not compare_all(s, ref), mode
     s.close()
 
 
