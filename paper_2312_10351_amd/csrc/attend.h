@@ -16,7 +16,7 @@
 // a fixed order, so the result does not depend on who that is.
 
 constexpr int attend_ring_bytes(int dp) { return 2 * 64 * dp; }      // of one wavefront: a tile of keys, one of values
-constexpr int lds_attend_rows(int dp) { return 4 * attend_ring_bytes(dp); }
+constexpr int lds_attend_rows(int dp, int waves) { return waves * attend_ring_bytes(dp); }
 
 constexpr float kAttendSlack = 8.f;
 
@@ -79,6 +79,21 @@ template <typename AR> struct AttendSight {
     return causal ? (int)max((int64_t)0, min((int64_t)length, i + ahead)) : length;
   }
 };
+
+// Which tile, share of its keys, key head and sequence a workgroup takes.  Every XCD takes a contiguous range of
+// them: its L2 then holds one head's keys for all tiles of query rows.  The tiles of a head in descending order:
+// under a causal mask the later rows have more to do.
+template <typename AR>
+__device__ __forceinline__ void attend_place(const AR &a, const Blk &b, int &tile, int &split, int &g, int &z) {
+  const uint32_t total = (uint32_t)(b.gx * b.gy * a.batch), lin = (uint32_t)b.lin + (uint32_t)(b.gx * b.gy) * (uint32_t)b.z;
+  const uint32_t xcd = lin % 8u, r = total % 8u, at = xcd * (total / 8u) + (xcd < r ? xcd : r) + lin / 8u;
+  const uint32_t head = at / (uint32_t)b.gx;
+  const int x = b.gx - 1 - (int)(at - head * (uint32_t)b.gx);
+  z = (int)(head / (uint32_t)b.gy);
+  g = (int)(head - (uint32_t)z * (uint32_t)b.gy);
+  tile = (int)fast_div((uint32_t)x, (uint32_t)a.splits, a.div_splits);
+  split = x - tile * a.splits;
+}
 
 // Four result columns of one query row; `scale`: one over the sum of its probabilities.
 template <typename T, typename AR>
@@ -271,7 +286,10 @@ __device__ __forceinline__ void attend_join(const AR &a, int64_t tile_id, const 
   }
 }
 
-template <typename T, int DP, bool VEC, typename AR>
+// NW: wavefronts of a workgroup.  They share its keys without the cost of a join, so that few query rows over some
+// hundred keys are best served by as many as workgroup memory holds; longer ones by smaller workgroups, of which
+// more run at once.
+template <typename T, int DP, bool VEC, int NW, typename AR>
 __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsigned char *lds) {
   typedef typename Vec16<T>::type V;
   typedef V VU __attribute__((aligned(sizeof(T))));
@@ -284,8 +302,8 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
   static_assert(RING == 2 * TILE && 16 * PITCH * 4 + 128 <= RING, "ring of a wavefront");
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int grp = lane >> 4, r16 = lane & 15;
-  const int tile = (int)fast_div((uint32_t)b.x, (uint32_t)a.splits, a.div_splits), split = b.x - tile * a.splits;
-  const int g = b.y, z = b.z;
+  int tile, split, g, z;
+  attend_place(a, b, tile, split, g, z);
   const int r0 = tile * 16, rows = a.m * a.share;
   const int r = r0 + r16, qi = (int)fast_div((uint32_t)r, (uint32_t)a.share, a.div_share), head = g * a.share + r - qi * a.share;
   const AttendSight<AR> sight(a, z, (int)fast_div((uint32_t)min(rows - 1, r0 + 15), (uint32_t)a.share, a.div_share));
@@ -294,7 +312,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
   const int tiles = (sight.end + KT - 1) / KT;
   // Tiles go round the wavefronts of all workgroups that share them: what is read at a time lies together
   // (65536 keys of 8 heads beside each other, 32 splits: 53.2 us; in runs of tiles 61.1).
-  const int first = split * 4 + wave, step = 4 * a.splits;
+  const int first = split * NW + wave, step = NW * a.splits;
 
   V qf[NS];                                                 // query row r16, elements (s * 4 + grp) * VE ..
   {
@@ -454,7 +472,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
     }
   }
 
-  // ---- the four wavefronts meet
+  // ---- the wavefronts meet
   wait_loads<0>();                                          // no load may outlive its ring
   sum = row_sum(sum);
   float *part = (float *)ring, *stat = part + 16 * PITCH;   // result rows, then maxima and sums
@@ -462,14 +480,15 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
   for (int j = 0; j < NO; ++j) *(floatx4 *)(part + r16 * PITCH + j * 16 + grp * 4) = o[j];
   if (grp == 0) { stat[r16] = top; stat[16 + r16] = sum; }
   __syncthreads();
-  const int pr = t >> 4, pc = (t & 15) * 4;                 // this thread's row and first column
+  constexpr int TR = 4 * NW, RUN = 4 * TR;                  // threads per row, the columns that they take at a time
+  const int pr = t / TR, pc = t % TR * 4;                   // this thread's row and first column
   const float *wave0 = (const float *)lds;
   constexpr int WF = RING / 4;                              // floats from one wavefront's part to the next
-  float share[4], all = -INFINITY, total = 0.f;
+  float share[NW], all = -INFINITY, total = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) all = fmaxf(all, wave0[w * WF + 16 * PITCH + pr]);
+  for (int w = 0; w < NW; ++w) all = fmaxf(all, wave0[w * WF + 16 * PITCH + pr]);
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < NW; ++w) {
     const float mw = wave0[w * WF + 16 * PITCH + pr];
     share[w] = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - all);
     total += share[w] * wave0[w * WF + 16 * PITCH + 16 + pr];
@@ -478,14 +497,14 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
   auto joined = [&](int col) {
     floatx4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) v += *(const floatx4 *)(wave0 + w * WF + pr * PITCH + col) * share[w];
+    for (int w = 0; w < NW; ++w) v += *(const floatx4 *)(wave0 + w * WF + pr * PITCH + col) * share[w];
     return v;
   };
   if (a.splits == 1) {
     const float inverse = attend_inverse(total);
     if (row < rows)
 #pragma unroll
-      for (int c = 0; c < DP; c += 64)
+      for (int c = 0; c < DP; c += RUN)
         if (c + pc < a.v_width) attend_store<T>(a, g, z, row, c + pc, joined(c + pc), inverse);
     return;
   }
@@ -493,13 +512,14 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
   float *slots = a.partials + tile_id * a.splits * (16 * DP + 32), *mineslot = slots + (int64_t)split * (16 * DP + 32);
   if (row < rows) {
 #pragma unroll
-    for (int c = 0; c < DP; c += 64) stg<true, floatx4>(mineslot + pr * DP + c + pc, joined(c + pc));
-    if ((t & 15) == 0) {
+    for (int c = 0; c < DP; c += RUN)
+      if (RUN <= DP || c + pc < DP) stg<true, floatx4>(mineslot + pr * DP + c + pc, joined(c + pc));
+    if (pc == 0) {
       stg<true, float>(mineslot + 16 * DP + pr, all);
       stg<true, float>(mineslot + 16 * DP + 16 + pr, total);
     }
   }
-  attend_join<T, DP, 16, 256>(a, tile_id, slots, g, z, r0, min(16, rows - r0) * (DP / 4), lds, [](int q, int &row, int &col) {
+  attend_join<T, DP, 16, 64 * NW>(a, tile_id, slots, g, z, r0, min(16, rows - r0) * (DP / 4), lds, [](int q, int &row, int &col) {
     row = q / (DP / 4);
     col = q % (DP / 4) * 4;
   });
@@ -528,19 +548,8 @@ __device__ __forceinline__ void attend_wide_body(const AR &a, const Blk &b, unsi
   constexpr int NS = DP / 32, NO = DP / 16;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int grp = lane >> 4, r16 = lane & 15;
-  // Every XCD takes a contiguous range of (sequence, key head, tile): its L2 then holds one head's keys.  The tiles
-  // of a head in descending order: under a causal mask the later rows have more to do.
   int tile, split, g, z;
-  {
-    const uint32_t total = (uint32_t)(b.gx * b.gy * a.batch), lin = (uint32_t)b.lin + (uint32_t)(b.gx * b.gy) * (uint32_t)b.z;
-    const uint32_t xcd = lin % 8u, r = total % 8u, at = xcd * (total / 8u) + (xcd < r ? xcd : r) + lin / 8u;
-    const uint32_t head = at / (uint32_t)b.gx;
-    const int x = b.gx - 1 - (int)(at - head * (uint32_t)b.gx);
-    z = (int)(head / (uint32_t)b.gy);
-    g = (int)(head - (uint32_t)z * (uint32_t)b.gy);
-    tile = (int)fast_div((uint32_t)x, (uint32_t)a.splits, a.div_splits);
-    split = x - tile * a.splits;
-  }
+  attend_place(a, b, tile, split, g, z);
   const int r0 = tile * (32 * NW), rows = a.m * a.share;
   int r[2], qi[2], mine[2];
   V qf[2][NS];

@@ -235,12 +235,16 @@ struct AttendArgs {
   X(attend_f16_rows256, AttendArgs)     \
   X(attend_f16_wide64, AttendArgs)      \
   X(attend_f16_wide128, AttendArgs)     \
+  X(attend_f16_deep64, AttendArgs)      \
+  X(attend_f16_deep128, AttendArgs)     \
   X(attend_f16_any64, AttendArgs)       \
   X(attend_f16_any128, AttendArgs)      \
   X(attend_f16_any256, AttendArgs)      \
   X(attend_f32_rows64, AttendArgs)      \
   X(attend_f32_rows128, AttendArgs)     \
   X(attend_f32_rows256, AttendArgs)     \
+  X(attend_f32_deep64, AttendArgs)      \
+  X(attend_f32_deep128, AttendArgs)     \
   X(attend_f32_any64, AttendArgs)       \
   X(attend_f32_any128, AttendArgs)      \
   X(attend_f32_any256, AttendArgs)

@@ -1670,16 +1670,25 @@ KDEF2(gated_f16_tile64, 256, 2, lds_tile(128, 64, 2), IgemmArgs, (gated_tile_bod
 KGATED(f16, half_t)
 KGATED(f32, float)
 #undef KGATED
-#define KATTEND(tn, T, dp)                                                                                    \
-  KDEF(attend_##tn##_rows##dp, 256, lds_attend_rows(dp), AttendArgs, (attend_rows_body<T, dp, true>(a, b, lds))) \
-  KDEF(attend_##tn##_any##dp, 256, lds_attend_rows(dp), AttendArgs, (attend_rows_body<T, dp, false>(a, b, lds)))
-KATTEND(f16, half_t, 64)
-KATTEND(f16, half_t, 128)
-KATTEND(f16, half_t, 256)
-KATTEND(f32, float, 64)
-KATTEND(f32, float, 128)
-KATTEND(f32, float, 256)
+// Wavefronts per SIMD as workgroup memory and registers allow; without the bound the compiler moves results to and
+// from accumulation registers.
+#define KATTEND(tn, T, dp, waves)                                                                             \
+  KDEF2(attend_##tn##_rows##dp, 256, waves, lds_attend_rows(dp, 4), AttendArgs, (attend_rows_body<T, dp, true, 4>(a, b, lds))) \
+  KDEF2(attend_##tn##_any##dp, 256, waves, lds_attend_rows(dp, 4), AttendArgs, (attend_rows_body<T, dp, false, 4>(a, b, lds)))
+KATTEND(f16, half_t, 64, 4)
+KATTEND(f16, half_t, 128, 2)
+KATTEND(f16, half_t, 256, 1)
+KATTEND(f32, float, 64, 4)
+KATTEND(f32, float, 128, 2)
+KATTEND(f32, float, 256, 1)
 #undef KATTEND
+#define KDEEP(tn, T, dp, waves) \
+  KDEF2(attend_##tn##_deep##dp, 64 * waves, waves / 4, lds_attend_rows(dp, waves), AttendArgs, (attend_rows_body<T, dp, true, waves>(a, b, lds)))
+KDEEP(f16, half_t, 64, 8)
+KDEEP(f16, half_t, 128, 8)
+KDEEP(f32, float, 64, 8)
+KDEEP(f32, float, 128, 8)
+#undef KDEEP
 KDEF2(attend_f16_wide64, 256, 2, lds_attend_wide(64), AttendArgs, (attend_wide_body<64, 4>(a, b, lds)))
 KDEF2(attend_f16_wide128, 256, 2, lds_attend_wide(128), AttendArgs, (attend_wide_body<128, 4>(a, b, lds)))
 

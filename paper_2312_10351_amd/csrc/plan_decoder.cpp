@@ -178,7 +178,7 @@ int plan_gated(const opara_op_desc &op, const opara_op_more &q, const void *cons
 
 // ---- attention
 struct AttendShape {
-  int64_t batch, heads, kv_heads, share, v_width, strides[4][3];
+  int64_t batch, heads, kv_heads, share, width, v_width, strides[4][3];
   int dp;                                  // both widths padded: 64, 128 or 256
   double keys;                             // what a query row sees of n in the mean, as far as the host knows
 };
@@ -188,6 +188,7 @@ int attend_shape(const opara_op_desc &op, const opara_op_more &q, AttendShape *s
   s->batch = p.batch ? p.batch : 1;
   s->heads = q.heads;
   s->kv_heads = q.kv_heads ? q.kv_heads : q.heads;
+  s->width = q.width;
   s->v_width = q.v_width ? q.v_width : q.width;
   if (s->batch < 1 || s->batch > 65535 || p.m <= 0 || p.n <= 0 || s->heads <= 0 || s->kv_heads <= 0 || s->heads % s->kv_heads)
     return fail("bad attention shape", op);
@@ -225,22 +226,33 @@ int attend_shape(const opara_op_desc &op, const opara_op_more &q, AttendShape *s
   return OPARA_OK;
 }
 
-// What the forms of attention cost: nanoseconds per key for a workgroup with a compute unit to itself (`alone`) and in
-// a full launch (`busy`), microseconds outside the keys (`fixed`), of a join of several workgroups
-// (`join`) and of every workgroup that is joined (`each`); records pass through memory at 2.5 TB/s.  Fitted to
-// 700 launches per type (1..2048 rows of 1..32 key heads, 128..65536 keys, 1..256 splits); the form and split it
-// picks are 2 % slower than the best in the mean.
-struct AttendForm { int kernel, any, rows, key_tile; double alone, busy, fixed, join, each; };   // any: for unaligned keys, -1 none
-const AttendForm kAttendF16[3][2] = {
-    {{K_attend_f16_rows64, K_attend_f16_any64, 16, 128, 7.3, 6.3, 3.1, 5.5, 0.10},
-     {K_attend_f16_wide64, -1, 128, 64, 16.9, 11.7, 3.4, 2.4, 0.63}},
-    {{K_attend_f16_rows128, K_attend_f16_any128, 16, 128, 8.3, 11.5, 4.2, 5.0, 0.25},
-     {K_attend_f16_wide128, -1, 128, 64, 26.9, 21.1, 4.3, 3.5, 0.90}},
-    {{K_attend_f16_rows256, K_attend_f16_any256, 16, 128, 16.0, 22.0, 6.0, 5.0, 0.27},
-     {-1, -1, 0, 0, 0, 0, 0, 0, 0}}};
-const AttendForm kAttendF32[3] = {{K_attend_f32_rows64, K_attend_f32_any64, 16, 64, 18.4, 17.9, 3.1, 5.8, 0.085},
-                                  {K_attend_f32_rows128, K_attend_f32_any128, 16, 64, 28.9, 34.7, 4.2, 5.7, 0.21},
-                                  {K_attend_f32_rows256, K_attend_f32_any256, 16, 64, 54.1, 80.0, 6.6, 5.0, 0.27}};
+// What the forms of attention cost: nanoseconds per key for a workgroup with a compute unit to itself whose keys are in
+// a cache (`alone`) or, all of them more than kAttendCached, come from memory (`far`), and in a full launch (`busy`);
+// microseconds of the launch and everything else outside the keys (`fixed`), of every further 256 workgroups
+// (`each`), of a join (`join`), of every workgroup that a tile is joined from (`part`) and of every 256 that leave a
+// record (`records`).  Fitted to about 1000 launches per type and width (1..2048 rows of 1..32 key heads,
+// 128..65536 keys, 1..256 splits) within 5 to 17 %; the form and split it picks are 2 % slower than the best in the mean.
+// The deep forms (eight wavefronts) against four: 12 heads of 64, 1500 keys, one row 8.0 -> 7.3 us, fp32, 4 x 77 rows,
+// 512 keys 11.5 -> 10.7; where many run at once the small ones are the faster, 1024 rows, 512 keys 9.4 and 11.9.
+struct AttendForm {
+  int kernel, any, rows, key_tile, threads;                 // any: for unaligned keys, -1 none
+  double alone, far, busy, fixed, each, join, part, records;
+};
+constexpr double kAttendCached = 85e6;
+const AttendForm kAttendF16[3][3] = {
+    {{K_attend_f16_rows64, K_attend_f16_any64, 16, 128, 256, 3.7, 6.7, 3.1, 3.7, 0.39, 2.4, 0.080, 1.7},
+     {K_attend_f16_deep64, -1, 16, 256, 512, 2.4, 6.6, 3.1, 4.0, 0.79, 3.7, 0.027, 2.9},
+     {K_attend_f16_wide64, -1, 128, 64, 256, 13.7, 14.0, 10.4, 4.5, 0.79, 2.9, 0.440, 1.9}},
+    {{K_attend_f16_rows128, K_attend_f16_any128, 16, 128, 256, 4.9, 10.9, 6.5, 4.7, 0.95, 2.3, 0.095, 1.9},
+     {K_attend_f16_deep128, -1, 16, 256, 512, 4.9, 10.6, 7.0, 4.4, 1.80, 3.6, 0.038, 4.5},
+     {K_attend_f16_wide128, -1, 128, 64, 256, 21.2, 21.2, 16.6, 5.8, 1.78, 3.1, 0.804, 3.7}},
+    {{K_attend_f16_rows256, K_attend_f16_any256, 16, 128, 256, 16.0, 16.0, 22.0, 6.0, 2.50, 2.5, 0.150, 3.0}}};
+const AttendForm kAttendF32[3][3] = {
+    {{K_attend_f32_rows64, K_attend_f32_any64, 16, 64, 256, 12.3, 13.4, 10.6, 4.1, 0.48, 2.4, 0.082, 1.2},
+     {K_attend_f32_deep64, -1, 16, 128, 512, 9.4, 11.0, 10.5, 4.6, 1.22, 3.7, 0.031, 1.7}},
+    {{K_attend_f32_rows128, K_attend_f32_any128, 16, 64, 256, 20.9, 21.1, 21.8, 5.0, 1.17, 2.7, 0.093, 1.2},
+     {K_attend_f32_deep128, -1, 16, 128, 512, 16.9, 19.5, 21.5, 5.5, 3.27, 3.7, 0.052, 2.8}},
+    {{K_attend_f32_rows256, K_attend_f32_any256, 16, 64, 256, 43.3, 43.3, 50.6, 7.6, 4.97, 1.9, 0.146, 1.0}}};
 
 struct AttendPick { const AttendForm *form; int64_t tiles, splits, counter_bytes, scratch; };
 
@@ -248,12 +260,13 @@ struct AttendPick { const AttendForm *form; int64_t tiles, splits, counter_bytes
 AttendPick attend_pick(const opara_op_desc &op, const AttendShape &s, bool vec, uint64_t room) {
   const bool f16 = op.dtype == OPARA_F16;
   const int size = s.dp == 64 ? 0 : s.dp == 128 ? 1 : 2;
-  const AttendForm *forms = f16 ? kAttendF16[size] : &kAttendF32[size];
+  const AttendForm *forms = f16 ? kAttendF16[size] : kAttendF32[size];
+  const double bytes = s.batch * s.kv_heads * s.keys * (s.width + s.v_width) * (f16 ? 2 : 4);
   AttendPick best{};
   double least = 0.0;
-  for (int i = 0; i < (f16 ? 2 : 1); ++i) {
+  for (int i = 0; i < 3 && forms[i].rows; ++i) {
     const AttendForm &f = forms[i];
-    if (f.kernel < 0 || (!vec && f.any < 0)) continue;
+    if (!vec && f.any < 0) continue;
     const int64_t tiles = cdiv((int64_t)op.params.m * s.share, f.rows), work = tiles * s.kv_heads * s.batch;
     for (int64_t n = 1; n <= kAttendMaxSplits; n = n < 4 ? n + 1 : n + n / 2) {
       if (n > 1 && n * f.key_tile > s.keys) break;           // two tiles for every wavefront
@@ -262,9 +275,11 @@ AttendPick attend_pick(const opara_op_desc &op, const AttendShape &s, bool vec, 
       const int64_t records = work * n * (f.rows * s.dp + 2 * f.rows) * 4;
       if (n > 1) p.scratch = p.counter_bytes + records;
       if ((uint64_t)p.scratch > room || p.scratch > kAttendMaxScratch) break;
-      const double keys = std::ceil(s.keys / (f.key_tile * n)) * f.key_tile;
-      double cost = f.fixed + std::max(keys * f.alone, work * n * keys / 256.0 * f.busy) * 1e-3;
-      if (n > 1) cost += f.join + f.each * n + records / 2.5e6;
+      const double keys = std::ceil(s.keys / (f.key_tile * n)) * f.key_tile, groups = work * n;
+      // Between one and four workgroups per compute unit the fuller ones decide, half of the time.
+      const double per_cu = groups > 256 && groups < 1024 ? 0.5 * (std::ceil(groups / 256) + groups / 256) : groups / 256;
+      double cost = f.fixed + std::max({keys * (bytes > kAttendCached ? f.far : f.alone) * 1e-3, per_cu * (keys * f.busy * 1e-3 + f.each), bytes / 6e6});
+      if (n > 1) cost += f.join + f.part * n + f.records * groups / 256;
       if (!best.form || cost < least) { best = p; least = cost; }
     }
   }
@@ -313,7 +328,7 @@ int plan_attention(const opara_op_desc &op, const opara_op_more &q, const void *
   out->kernel = vec ? pick.form->kernel : pick.form->any;
   const int64_t gx = pick.tiles * pick.splits;
   if (gx * s.kv_heads * s.batch > kInt) return too_large("more rows than one launch holds", op);
-  out->gx = (uint32_t)gx; out->gy = (uint32_t)s.kv_heads; out->gz = (uint32_t)s.batch; out->block = 256;
+  out->gx = (uint32_t)gx; out->gy = (uint32_t)s.kv_heads; out->gz = (uint32_t)s.batch; out->block = (uint32_t)(vec ? pick.form->threads : 256);
   out->args.attend = a;
   return OPARA_OK;
 }

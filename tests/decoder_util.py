@@ -55,6 +55,11 @@ ATTEND = [
     (3, 1500, 400, 24, 8, 96, 128, [400, 0, 77], None, 0),
     (2, 40, 300, 4, 2, 101, 77, [300, 222], "end", 0),
     (1, 300, 12000, 7, 1, 128, 128, None, "start", 11650),
+    (1, 1000, 1000, 24, 8, 64, 64, None, "start", 0),
+    (2, 600, 5000, 6, 1, 64, 56, [5000, 3], None, 0),
+    (1, 70, 700, 4, 4, 128, 104, [680], "end", 0),
+    (1, 200, 6000, 2, 1, 64, 64, None, "end", 0),
+    (1, 1, 1500, 12, 4, 128, 128, [1499], None, 0),
 ]
 
 

@@ -263,7 +263,8 @@ def test_attention_lengths_are_read_at_every_launch():
 
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
 @pytest.mark.parametrize("m, heads, kv, width, causal", [(20, 2, 1, 64, "start"), (1000, 8, 4, 128, "start"), (900, 8, 8, 64, "end"), (70, 2, 2, 37, "start"),
-                                                         (33, 1, 1, 256, "end"), (129, 3, 3, 130, "start")])
+                                                         (33, 1, 1, 256, "end"), (129, 3, 3, 130, "start"), (1000, 24, 8, 64, "start"),
+                                                         (1300, 8, 4, 128, "start"), (2000, 8, 4, 64, "end")])
 def test_attention_of_rows_that_do_not_see_what_is_not_finite(dtype, m, heads, kv, width, causal):
     """Under a causal mask later keys and values may hold anything: rows before them are as without them."""
     first, second = m // 3, m * 2 // 3
