@@ -9,11 +9,17 @@
 // Statistics and sums are fp32.  Probabilities are rounded to the element type for the matrix cores:
 // relative 2^-11 per term in fp16, as the result's own rounding; their sum is taken before that.
 //
-// rows kernels: sixteen query rows per workgroup, keys dealt to its four wavefronts in tiles of KT;
+// rows kernels: sixteen query rows per workgroup, keys dealt to its four (deep: eight) wavefronts in tiles of KT;
 // each wavefront has its own ring in workgroup memory and its own maximum, sum and result, which meet at
 // the end.  Where there are few query rows the keys of a tile are also shared out between `splits`
 // workgroups: each leaves (maximum, sum, result) in scratch memory and the last to arrive joins them in
 // a fixed order, so the result does not depend on who that is.
+// What bounds them: few rows over many keys the keys' bytes (fp16, 32 heads over 8 of 128, 65536 keys, one row:
+// 54.6 us, 4.9 TB/s, a large copy runs at 4.9); few rows over few keys latencies, launch, first loads and
+// join (12 heads of 64, 1500 keys: 7.2 us, of which an empty launch takes 2.2); many rows in fp32 the matrix
+// cores (32 heads over 8 of 128, causal, 2048 rows: 335 us, 103 TFLOP/s, a large matrix product reaches 154).
+// Lanes hold whole rows of scores in registers: one wavefront works on a tile for about 1 us, 0.4 of it matrix
+// instructions, so that several per SIMD are wanted.
 
 constexpr int attend_ring_bytes(int dp) { return 2 * 64 * dp; }      // of one wavefront: a tile of keys, one of values
 constexpr int lds_attend_rows(int dp, int waves) { return waves * attend_ring_bytes(dp); }
@@ -534,8 +540,8 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
 // with 32 x 32 ones, which need half as many reductions, the same kernel measured 9 % slower.
 // The result is scaled down only when a row's maximum has grown by more than 2^kAttendSlack: until
 // then probabilities may exceed one, by at most that, which their rounding, relative to each, does not see.
-// Measured, fp16, 32 heads over 8 of 128, 8192 rows (us): causal 573 (960 TFLOP/s), all keys 1094 (1005; without the
-// softmax 1050, a large matrix product reaches 1350); 16 heads of 64, 4096 rows 93 (738).
+// Measured, fp16, 32 heads over 8 of 128, 8192 rows (us): causal 551 (997 TFLOP/s), all keys 1093 (1006; without the
+// softmax 1050, a large matrix product reaches 1350); 16 heads of 64, 4096 rows 90 (762).
 constexpr int lds_attend_wide(int dp) { return 4 * 64 * dp * 2; }
 
 template <int DP, int NW, typename AR>

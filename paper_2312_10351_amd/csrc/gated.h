@@ -7,7 +7,7 @@
 //
 // What bounds it: with few rows the weights' bytes, with many the matrix cores.  Measured, fp16, 4096 -> 2 x 12288
 // (us; the plain library product of the same size reaches 1350 TFLOP/s): 1 row 34.4 (5.9 TB/s of weights),
-// 64 rows 48, 512 rows 109, 4096 rows 660 (1250 TFLOP/s).  Which form runs follows from a table of costs
+// 64 rows 48, 512 rows 109, 4096 rows 680 (1210 TFLOP/s).  Which form runs follows from a table of costs
 // (kGatedForms in plan_decoder.cpp).
 
 template <typename T> __device__ __forceinline__ float gate_apply(int act, float x) {
@@ -50,22 +50,31 @@ __device__ __forceinline__ void gated_store4(const AR &a, floatx4 g, floatx4 u, 
 
 // Any row length, alignment and operand size: 64 rows x 32 columns per workgroup, operands staged
 // through registers at element alignment and with 64-bit addresses.
+constexpr int kGatedAnyRow = 144;                          // bytes from one row of a tile to the next: 128 and a skew
 template <typename T, typename AR>
 __device__ __forceinline__ void gated_any_body(const AR &a, const Blk &b, unsigned char *lds) {
   typedef typename Vec16<T>::type V;
   typedef V VU __attribute__((aligned(sizeof(T))));
-  constexpr int VE = Vec16<T>::N, BKE = 4 * VE, ROWB = 80, BM = 64, BC = 32;
+  constexpr int VE = Vec16<T>::N, BKE = 8 * VE, ROWB = kGatedAnyRow, BM = 64, BC = 32;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, grp = lane >> 4, r16 = lane & 15;
   int tile_x, tile_y;
   xcd_tile(b, a.div_gx, tile_x, tile_y);
   const int m0 = tile_x * BM, n0 = tile_y * BC;
-  const int kc = t & 3, row = t >> 2;                       // 16-byte chunk and tile row this thread moves
-  // tile rows 0..31: gate columns, 32..63: the values they multiply
-  const int n = n0 + (row & 31), m = m0 + row;
-  const T *wr = (const T *)a.w + ((int64_t)(row >> 5) * a.N + min(n, a.N - 1)) * a.ldb;
-  const T *xr = (const T *)a.x + (int64_t)min(m, a.M - 1) * a.lda;
-  const bool wok = n < a.N, xok = m < a.M;
-  V wv, xv;
+  // A thread moves a 16-byte chunk of rows `row` and `row` + 32: a gate column and the value it is
+  // multiplied with, two rows of the input.  128 bytes of every row per step: with 64 the loads' latency is paid twice as often
+  // (fp16, 77 x 1001 x 2000 21.5 -> 16.4 us, 2000 x 1001 x 2000 58.5 -> 54.5; fp32, 300 x 999 x 2000 52.5 -> 49.0,
+  // 2000 x 999 x 2000 174 -> 177).
+  const int kc = t & 7, row = t >> 3, n = n0 + row;
+  const T *wr[2], *xr[2];
+  bool xok[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    wr[h] = (const T *)a.w + ((int64_t)h * a.N + min(n, a.N - 1)) * a.ldb;
+    xr[h] = (const T *)a.x + (int64_t)min(m0 + row + h * 32, a.M - 1) * a.lda;
+    xok[h] = m0 + row + h * 32 < a.M;
+  }
+  const bool wok = n < a.N;
+  V wv[2], xv[2];
   auto load = [&](const T *p, bool ok, int k) {
     V v = {};
     if (ok && k + VE <= a.K) v = *(const VU *)(p + k);
@@ -76,28 +85,37 @@ __device__ __forceinline__ void gated_any_body(const AR &a, const Blk &b, unsign
     return v;
   };
   unsigned char (*smem)[2 * 64 * ROWB] = (unsigned char (*)[2 * 64 * ROWB])lds;      // [2][weights, rows]
+  auto fetch = [&](int kt) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      wv[h] = load(wr[h], wok, kt * BKE + kc * VE);
+      xv[h] = load(xr[h], xok[h], kt * BKE + kc * VE);
+    }
+  };
   auto put = [&](int buf) {
-    *(V *)(smem[buf] + row * ROWB + kc * 16) = wv;
-    *(V *)(smem[buf] + (64 + row) * ROWB + kc * 16) = xv;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      *(V *)(smem[buf] + (row + h * 32) * ROWB + kc * 16) = wv[h];
+      *(V *)(smem[buf] + (64 + row + h * 32) * ROWB + kc * 16) = xv[h];
+    }
   };
   floatx4 acc[4];                                           // gate, gate, value, value columns of this wavefront's 16 rows
 #pragma unroll
   for (int i = 0; i < 4; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
   const int nk = (a.K + BKE - 1) / BKE;
-  wv = load(wr, wok, kc * VE);
-  xv = load(xr, xok, kc * VE);
+  fetch(0);
   put(0);
   __syncthreads();
   for (int kt = 0; kt < nk; ++kt) {
     const bool more = kt + 1 < nk;
-    if (more) {
-      wv = load(wr, wok, (kt + 1) * BKE + kc * VE);
-      xv = load(xr, xok, (kt + 1) * BKE + kc * VE);
-    }
+    if (more) fetch(kt + 1);
     const unsigned char *W = smem[kt & 1], *X = W + 64 * ROWB;
-    const V xf = *(const V *)(X + (wave * 16 + r16) * ROWB + grp * 16);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] = mma16<T>(*(const V *)(W + (i * 16 + r16) * ROWB + grp * 16), xf, acc[i]);
+    for (int s = 0; s < 2; ++s) {
+      const V xf = *(const V *)(X + (wave * 16 + r16) * ROWB + (s * 4 + grp) * 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i] = mma16<T>(*(const V *)(W + (i * 16 + r16) * ROWB + (s * 4 + grp) * 16), xf, acc[i]);
+    }
     if (more) put((kt & 1) ^ 1);
     __syncthreads();
   }

@@ -1491,7 +1491,7 @@ constexpr int lds_tile(int bn, int bm, int stages) { return stages * (bn + bm) *
 constexpr int lds_split(int ni, int nj, int s) { return 4 * split_ring_bytes(ni, nj, s); }
 constexpr int lds_direct(int waves) { return waves * 32 * 36 * 4; }
 constexpr int kLdsGap = 4 * 64 * 4, kLdsRow = 16, kLdsNone = 0;
-constexpr int kLdsGatedAny = 2 * 2 * 64 * 80;
+constexpr int kLdsGatedAny = 2 * 2 * 64 * kGatedAnyRow;
 // ... of the bodies that group and chained kernels hold: the most a node of theirs asks for.
 constexpr int kLdsLargestBody = std::max({lds_igemm(64, 64), lds_tile(128, 128, 2), lds_tile(64, 64, 3), lds_tile(128, 64, 2),
                                           lds_split(1, 1, 3), lds_split(2, 2, 2), lds_split(4, 2, 1), lds_split(4, 4, 1), lds_direct(4)});
@@ -1657,8 +1657,8 @@ DECODER_BODIES(KDECODER, float, f32)
 #undef KDECODER
 KDEF2(resnorm_f16_huge, 256, 1, kLdsRow, NormArgs, (residual_norm_body<half_t, 256, kNormHugePieces, 8, false>(a, b, lds)))
 KDEF2(resnorm_f32_huge, 256, 2, kLdsRow, NormArgs, (residual_norm_body<float, 256, kNormHugePieces, 4, false>(a, b, lds)))
-KDEF(gated_f16_any, 256, kLdsGatedAny, IgemmArgs, (gated_any_body<half_t>(a, b, lds)))
-KDEF(gated_f32_any, 256, kLdsGatedAny, IgemmArgs, (gated_any_body<float>(a, b, lds)))
+KDEF2(gated_f16_any, 256, 4, kLdsGatedAny, IgemmArgs, (gated_any_body<half_t>(a, b, lds)))
+KDEF2(gated_f32_any, 256, 4, kLdsGatedAny, IgemmArgs, (gated_any_body<float>(a, b, lds)))
 KDEF2(gated_f16_tile256, 512, 2, lds_tile(256, 256, 2), IgemmArgs, (gated_wide_body<256, 256, 4, 2>(a, b, lds)))
 #define KGATED(tn, T)                                                                                         \
   KDEF(gated_##tn##_row, 256, kLdsNone, IgemmArgs, (gated_row_body<T>(a, b, lds)))                             \
