@@ -1649,7 +1649,7 @@ KDEF2(attention_f16, 256, 2, kLdsAttention, AttnArgs, (attention_body(a, b, lds)
   X(resnorm_##tn##_block, NormArgs, 4, (residual_norm_body<T, 256, kNormBlockPieces, Vec16<T>::N, true>(a, b, lds)))  \
   X(resnorm_##tn##_large, NormArgs, 2, (residual_norm_body<T, 256, kNormLargePieces, Vec16<T>::N, false>(a, b, lds))) \
   X(resnorm_##tn##_odd, NormArgs, 4, (residual_norm_body<T, 256, kNormOddPieces, 1, true>(a, b, lds)))        \
-  X(resnorm_##tn##_oddlarge, NormArgs, 4, (residual_norm_body<T, 256, 2 * kNormOddPieces, 1, false>(a, b, lds))) \
+  X(resnorm_##tn##_oddlarge, NormArgs, 2, (residual_norm_body<T, 256, 2 * kNormOddPieces, 1, false>(a, b, lds))) \
   X(resnorm_##tn##_wide, NormArgs, 4, (residual_norm_wide_body<T>(a, b, lds)))
 #define KDECODER(name, Args, waves, call) KDEF2(name, 256, waves, kLdsRow, Args, call)
 DECODER_BODIES(KDECODER, half_t, f16)
