@@ -26,11 +26,20 @@ constexpr int lds_attend_rows(int dp, int waves) { return waves * attend_ring_by
 
 constexpr float kAttendSlack = 8.f;
 
-// L loads of a wavefront bring its share of a tile of KT keys (or values) straight into workgroup memory.  A row's chunk
-// c lies in slot c ^ (row & 7): fragment reads of adjacent rows then differ in their banks.  Offsets inside a
+// A row's 16-byte chunk c lies in slot c ^ attend_slot(row), so that what one fragment read takes at a time lies in
+// different banks: of keys one chunk of 8 rows; of values in fp16 (read transposed) two chunks of 8 rows, in
+// 256 bytes, in fp32 four chunks of every fourth row.  (With the keys' form for both every transposed read took
+// twice its time: SQ_LDS_BANK_CONFLICT was 23 % of the busy cycles of the wide kernel.)
+template <typename T, int DP, bool VALUES> __device__ __forceinline__ constexpr int attend_slot(int row) {
+  if constexpr (!VALUES) return row & 7;
+  else if constexpr (sizeof(T) == 4) return (row >> 2 & 3) << 2;
+  else return DP == 64 ? (row >> 1 & 3) << 1 : (row & 7) << 1;
+}
+
+// L loads of a wavefront bring its share of a tile of KT keys (or values) straight into workgroup memory.  Offsets inside a
 // tile are worked out once; a tile is a buffer that begins at its first row and ends with the last key, so
 // rows behind that arrive as zeros, and a step costs no vector instruction but the loads.
-template <typename T, int DP, int KT, int L> struct KeyStager {
+template <typename T, int DP, int KT, int L, bool VALUES> struct KeyStager {
   static constexpr int ES = (int)sizeof(T), CH = DP * ES / 16, RL = 64 / CH;     // chunks per row, rows per load
   uint32_t off[L], row_bytes;
   const unsigned char *at;
@@ -39,7 +48,7 @@ template <typename T, int DP, int KT, int L> struct KeyStager {
   __device__ __forceinline__ void init(const T *base, int64_t pitch, int width, int share, int first_tile, int tiles, int lane) {
 #pragma unroll
     for (int l = 0; l < L; ++l) {
-      const int row = (share * L + l) * RL + lane / CH, d = ((lane % CH) ^ (row & 7)) * (16 / ES);
+      const int row = (share * L + l) * RL + lane / CH, d = ((lane % CH) ^ attend_slot<T, DP, VALUES>(row)) * (16 / ES);
       off[l] = d < width ? ((uint32_t)row * (uint32_t)pitch + (uint32_t)d) * ES : kOperandMaxBytes;
     }
     row_bytes = (uint32_t)pitch * ES;
@@ -144,7 +153,7 @@ __device__ __forceinline__ void add_infinite(const unsigned char *tile, int firs
 #pragma unroll
     for (int j = 0; j < DP / 16; ++j) {
       const int byte = (j * 16 + grp * 4) * ES;
-      const R v = *(const R *)(tile + key * (DP * ES) + (((byte >> 4) ^ (key & 7)) << 4) + (byte & 15));
+      const R v = *(const R *)(tile + key * (DP * ES) + (((byte >> 4) ^ attend_slot<T, DP, true>(key)) << 4) + (byte & 15));
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float f = (float)v[e], add = fabsf(f) < INFINITY ? 0.f : f;
@@ -339,17 +348,18 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
   }
   const T *kbase = (const T *)a.k + z * a.k_s[0] + g * a.k_s[2], *vbase = (const T *)a.v + z * a.v_s[0] + g * a.v_s[2];
   unsigned char *ring = lds + wave * RING;                  // a tile of keys, a tile of values
-  typedef KeyStager<T, DP, KT, L> Stage;
-  Stage keys, values;
+  KeyStager<T, DP, KT, L, false> keys;
+  KeyStager<T, DP, KT, L, true> values;
   if constexpr (VEC) {
     keys.init(kbase, a.k_s[1], a.width, 0, first, step, lane);
     values.init(vbase, a.v_s[1], a.v_width, 0, first, step, lane);
   }
   // Rows at any address and distance: through registers.
-  auto copy = [&](const T *base, int64_t pitch, int width, int kt, unsigned char *to) {
+  auto copy = [&](const T *base, int64_t pitch, int width, int kt, unsigned char *to, auto values_tag) {
 #pragma unroll
     for (int l = 0; l < L; ++l) {
-      const int row = l * Stage::RL + lane / CH, key = kt * KT + row, d = ((lane % CH) ^ (row & 7)) * VE;
+      const int row = l * (64 / CH) + lane / CH, key = kt * KT + row;
+      const int d = ((lane % CH) ^ attend_slot<T, DP, decltype(values_tag)::value>(row)) * VE;
       V v = {};
       if (key < sight.end) {
         const T *src = base + (int64_t)key * pitch + d;
@@ -381,7 +391,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
   for (; kt < tiles; kt += step) {
     const int left = sight.end - (kt + step) * KT;          // of the tile after this one
     if constexpr (VEC) wait_loads<L>();
-    else copy(kbase, a.k_s[1], a.width, kt, ring);
+    else copy(kbase, a.k_s[1], a.width, kt, ring, std::false_type{});
     // ---- scores of KT keys
     floatx4 p[NQ];
     {
@@ -442,7 +452,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
       }
     // ---- O^T += V^T P^T; key e of a lane's step: 16 * (e / 4) + 4 * grp + e % 4
     if constexpr (VEC) wait_loads<L>();
-    else copy(vbase, a.v_s[1], a.v_width, kt, ring + TILE);
+    else copy(vbase, a.v_s[1], a.v_width, kt, ring + TILE, std::true_type{});
     const unsigned char *W = ring + TILE;
     V pf;
 #pragma unroll
@@ -453,7 +463,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int row = h * 16 + grp * 4 + (r16 >> 2);
-          v[h] = lds_read_transposed(W + row * (DP * ES) + (((j * 2 + ((r16 >> 1) & 1)) ^ (row & 7)) * 16) + (r16 & 1) * 8);
+          v[h] = lds_read_transposed(W + row * (DP * ES) + (((j * 2 + ((r16 >> 1) & 1)) ^ attend_slot<T, DP, true>(row)) * 16) + (r16 & 1) * 8);
         }
         return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
       } else {
@@ -461,7 +471,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int row = grp * 4 + e;
-          v[e] = *(const T *)(W + row * (DP * ES) + (((j * 4 + (r16 >> 2)) ^ (row & 7)) * 16) + (r16 & 3) * 4);
+          v[e] = *(const T *)(W + row * (DP * ES) + (((j * 4 + (r16 >> 2)) ^ attend_slot<T, DP, true>(row)) * 16) + (r16 & 3) * 4);
         }
         return v;
       }
@@ -585,7 +595,8 @@ __device__ __forceinline__ void attend_wide_body(const AR &a, const Blk &b, unsi
       qf[x][s] = a.negative ? -v : v;
     }
   }
-  KeyStager<T, DP, KT, L> keys, values;
+  KeyStager<T, DP, KT, L, false> keys;
+  KeyStager<T, DP, KT, L, true> values;
   keys.init((const T *)a.k + z * a.k_s[0] + g * a.k_s[2], a.k_s[1], a.width, wave, split, a.splits, lane);
   values.init((const T *)a.v + z * a.v_s[0] + g * a.v_s[2], a.v_s[1], a.v_width, wave, split, a.splits, lane);
   const uint32_t base = lds_address(lds) + wave * L * 1024;
@@ -661,7 +672,7 @@ __device__ __forceinline__ void attend_wide_body(const AR &a, const Blk &b, unsi
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int row = q * 32 + h * 16 + grp * 4 + (r16 >> 2), chunk = j * 2 + ((r16 >> 1) & 1);
-      v[h] = lds_read_transposed(lds + (2 + slot) * TILE + row * (DP * 2) + ((chunk ^ (row & 7)) * 16) + (r16 & 1) * 8);
+      v[h] = lds_read_transposed(lds + (2 + slot) * TILE + row * (DP * 2) + ((chunk ^ attend_slot<T, DP, true>(row)) * 16) + (r16 & 1) * 8);
     }
     return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
   };
