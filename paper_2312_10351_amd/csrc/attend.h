@@ -27,11 +27,11 @@ constexpr int lds_attend_rows(int dp, int waves) { return waves * attend_ring_by
 constexpr float kAttendSlack = 8.f;
 
 // A row's 16-byte chunk c lies in slot c ^ attend_slot(row), so that what one fragment read takes at a time lies in
-// different banks: of keys one chunk of 8 rows; of values in fp16 (read transposed) two chunks of 8 rows, in
-// 256 bytes, in fp32 four chunks of every fourth row.  (With the keys' form for both every transposed read took
+// different banks, which are 256 bytes wide: of keys one chunk of 16 rows; of values in fp16 (read transposed) two
+// chunks of 8 rows, in fp32 four chunks of every fourth row.  (With row & 7 for both, each read took
 // twice its time: SQ_LDS_BANK_CONFLICT was 23 % of the busy cycles of the wide kernel.)
 template <typename T, int DP, bool VALUES> __device__ __forceinline__ constexpr int attend_slot(int row) {
-  if constexpr (!VALUES) return row & 7;
+  if constexpr (!VALUES) return DP * sizeof(T) == 128 ? row >> 1 & 7 : row & 15;
   else if constexpr (sizeof(T) == 4) return (row >> 2 & 3) << 2;
   else return DP == 64 ? (row >> 1 & 3) << 1 : (row & 7) << 1;
 }
@@ -404,7 +404,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
           const int row = i * 16 + r16;
-          const V kf = *(const V *)(K + row * (DP * ES) + (((s * 4 + grp) ^ (row & 7)) * 16));
+          const V kf = *(const V *)(K + row * (DP * ES) + (((s * 4 + grp) ^ attend_slot<T, DP, false>(row)) * 16));
           if constexpr (ES == 2) {
             acc = mma16<T>(kf, qf[s], acc);
           } else {
@@ -620,7 +620,7 @@ __device__ __forceinline__ void attend_wide_body(const AR &a, const Blk &b, unsi
     for (int d = 0; d < NS; ++d)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const V kf = *(const V *)(K + (i * 16 + r16) * (DP * 2) + (((d * 4 + grp) ^ (r16 & 7)) * 16));
+        const V kf = *(const V *)(K + (i * 16 + r16) * (DP * 2) + (((d * 4 + grp) ^ attend_slot<T, DP, false>(r16)) * 16));
 #pragma unroll
         for (int x = 0; x < 2; ++x) s[i][x] = mma16<T>(kf, qf[x][d], s[i][x]);
       }
