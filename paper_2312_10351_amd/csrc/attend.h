@@ -17,7 +17,7 @@
 // What bounds them: few rows over many keys the keys' bytes (fp16, 32 heads over 8 of 128, 65536 keys, one row:
 // 54.6 us, 4.9 TB/s, a large copy runs at 4.9); few rows over few keys latencies, launch, first loads and
 // join (12 heads of 64, 1500 keys: 7.2 us, of which an empty launch takes 2.2); many rows in fp32 the matrix
-// cores (32 heads over 8 of 128, causal, 2048 rows: 335 us, 103 TFLOP/s, a large matrix product reaches 154).
+// cores (32 heads over 8 of 128, causal, 2048 rows: 322 us, 107 TFLOP/s, a large matrix product reaches 154).
 // Lanes hold whole rows of scores in registers: one wavefront works on a tile for about 1 us, 0.4 of it matrix
 // instructions, so that several per SIMD are wanted.
 
@@ -326,7 +326,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
   const int every = sight.limit((int)fast_div((uint32_t)r0, (uint32_t)a.share, a.div_share));      // every row sees these
   const int tiles = (sight.end + KT - 1) / KT;
   // Tiles go round the wavefronts of all workgroups that share them: what is read at a time lies together
-  // (65536 keys of 8 heads beside each other, 32 splits: 53.2 us; in runs of tiles 61.1).
+  // (65536 keys of 8 heads beside each other: 53.2 us; in runs of tiles 61.1).
   const int first = split * NW + wave, step = NW * a.splits;
 
   V qf[NS];                                                 // query row r16, elements (s * 4 + grp) * VE ..
@@ -550,8 +550,9 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
 // with 32 x 32 ones, which need half as many reductions, the same kernel measured 9 % slower.
 // The result is scaled down only when a row's maximum has grown by more than 2^kAttendSlack: until
 // then probabilities may exceed one, by at most that, which their rounding, relative to each, does not see.
-// Measured, fp16, 32 heads over 8 of 128, 8192 rows (us): causal 551 (997 TFLOP/s), all keys 1093 (1006; without the
-// softmax 1050, a large matrix product reaches 1350); 16 heads of 64, 4096 rows 90 (762).
+// Measured, fp16, 32 heads over 8 of 128, 8192 rows (us): causal 545 (1009 TFLOP/s), all keys 1031 (1066; a
+// large matrix product reaches 1350); 16 heads of 64, 4096 rows 88 (779).  Matrix cores busy 49 % of the
+// compute units' cycles (causal), 256 vector instructions for 64 matrix instructions of 16 cycles.
 constexpr int lds_attend_wide(int dp) { return 4 * 64 * dp * 2; }
 
 template <int DP, int NW, typename AR>

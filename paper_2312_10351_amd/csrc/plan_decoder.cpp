@@ -232,8 +232,9 @@ int attend_shape(const opara_op_desc &op, const opara_op_more &q, AttendShape *s
 // (`each`), of a join (`join`), of every workgroup that a tile is joined from (`part`) and of every 256 that leave a
 // record (`records`).  Fitted to about 1000 launches per type and width (1..2048 rows of 1..32 key heads,
 // 128..65536 keys, 1..256 splits) within 5 to 17 %; the form and split it picks are 2 % slower than the best in the mean.
-// The deep forms (eight wavefronts) against four: 12 heads of 64, 1500 keys, one row 8.0 -> 7.3 us, fp32, 4 x 77 rows,
-// 512 keys 11.5 -> 10.7; where many run at once the small ones are the faster, 1024 rows, 512 keys 9.4 and 11.9.
+// The deep forms (eight wavefronts) against four: 12 heads of 64, 1500 keys, one row 8.0 -> 7.2 us, one key head of 64,
+// 2048 rows, 4096 keys 16.8 -> 12.3; where many workgroups run at once the small ones are the faster, 12 heads of 64,
+// 1024 rows, 512 keys 11.9 and 9.4.
 struct AttendForm {
   int kernel, any, rows, key_tile, threads;                 // any: for unaligned keys, -1 none
   double alone, far, busy, fixed, each, join, part, records;
