@@ -7,7 +7,10 @@
 // of a row need two shuffles per tile, and its probabilities already lie where the second product wants them,
 // O^T += V^T P^T (both operands number the keys of a step alike, in whatever order).
 // Statistics and sums are fp32.  Probabilities are rounded to the element type for the matrix cores:
-// relative 2^-11 per term in fp16, as the result's own rounding; their sum is taken before that.
+// relative 2^-11 per term in fp16, as the result's own rounding; their sum is taken before that.  They are formed
+// 2^kAttendLift times too large, a factor that the sum has too: fp16 then keeps all bits of weights down to 2^-25 of a
+// row's largest, and below that multiples of 2^-35 of it.  (Without it weights below 2^-25 of the largest were lost,
+// which a tail of 2^16 keys and more shows.)
 //
 // rows kernels: sixteen query rows per workgroup, keys dealt to its four (deep: eight) wavefronts in tiles of KT;
 // each wavefront has its own ring in workgroup memory and its own maximum, sum and result, which meet at
@@ -24,7 +27,10 @@
 constexpr int attend_ring_bytes(int dp) { return 2 * 64 * dp; }      // of one wavefront: a tile of keys, one of values
 constexpr int lds_attend_rows(int dp, int waves) { return waves * attend_ring_bytes(dp); }
 
-constexpr float kAttendSlack = 8.f;
+// A result is scaled down only when its row's maximum has grown by more than 2^kAttendSlack.  Together the two stay below
+// fp16's largest power of two, 2^15.  A slack of 8 leaves 7 for the lift; for scores of standard deviation 1 (causal,
+// 8192 rows) it costs the same, of 8 it takes 525 us against 535.
+constexpr float kAttendSlack = 4.f, kAttendLift = 11.f;
 
 // A row's 16-byte chunk c lies in slot c ^ attend_slot(row), so that what one fragment read takes at a time lies in
 // different banks, which are 256 bytes wide: of keys one chunk of 16 rows; of values in fp16 (read transposed) two
@@ -432,7 +438,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
     for (int i = 0; i < NQ; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) most = fmaxf(most, p[i][e]);
-    most = row_max(most) * a.scale;                         // a positive factor
+    most = row_max(most) * a.scale - kAttendLift;           // a positive factor
     if (__any(most > top + kAttendSlack)) {
       const float now = fmaxf(most, top), shrink = __builtin_amdgcn_exp2f(top - (now == -INFINITY ? 0.f : now));
       top = now;
@@ -548,8 +554,6 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
 // a width of 128; exponentials take a quarter of the rate) and 16 KB of fragment reads each for keys and values; two
 // wavefronts per SIMD overlap the three, the one at a product first (s_setprio).  16 x 16 matrix instructions:
 // with 32 x 32 ones, which need half as many reductions, the same kernel measured 9 % slower.
-// The result is scaled down only when a row's maximum has grown by more than 2^kAttendSlack: until
-// then probabilities may exceed one, by at most that, which their rounding, relative to each, does not see.
 // Measured, fp16, 32 heads over 8 of 128, 8192 rows (us): causal 545 (1009 TFLOP/s), all keys 1031 (1066; a
 // large matrix product reaches 1350); 16 heads of 64, 4096 rows 88 (779).  Matrix cores busy 49 % of the
 // compute units' cycles (causal), 256 vector instructions for 64 matrix instructions of 16 cycles.
@@ -641,7 +645,7 @@ __device__ __forceinline__ void attend_wide_body(const AR &a, const Blk &b, unsi
           most[x] = fmaxf(most[x], s[i][x][e]);
         }
       if constexpr (!MASKED) most[x] *= a.scale;
-      most[x] = row_max(most[x]);
+      most[x] = row_max(most[x]) - kAttendLift;
     }
     if (__any(most[0] > top[0] + kAttendSlack || most[1] > top[1] + kAttendSlack)) {
 #pragma unroll
