@@ -6,11 +6,14 @@
 // transposed, S^T = K Q^T: a lane then holds one query row and a few keys of it, the maximum and sum
 // of a row need two shuffles per tile, and its probabilities already lie where the second product wants them,
 // O^T += V^T P^T (both operands number the keys of a step alike, in whatever order).
-// Statistics and sums are fp32.  Probabilities are rounded to the element type for the matrix cores:
-// relative 2^-11 per term in fp16, as the result's own rounding; their sum is taken before that.  They are formed
-// 2^kAttendLift times too large, a factor that the sum has too: fp16 then keeps all bits of weights down to 2^-25 of a
-// row's largest, and below that multiples of 2^-35 of it.  (Without it weights below 2^-25 of the largest were lost,
-// which a tail of 2^16 keys and more shows.)
+// Statistics and sums are fp32.  The matrix cores take probabilities of the element type, in fp16 rounded by relative
+// 2^-11, while their sum is taken before that.  They are formed 2^kAttendLift times too large, a factor that the sum
+// has too: fp16 then keeps all bits of weights down to 2^-25 of a row's largest, and below that multiples of 2^-35 of
+// it.  (Without it weights below 2^-25 of the largest were lost, which a tail of 2^16 keys and more shows.)
+// What the rounding takes off a probability is an fp16 number too (but for 2^-20 of the probability), and a second
+// product adds it where bytes and latencies are the bound, in the rows kernels: a result is then off by its own rounding alone (1500 keys, root mean square
+// against 64 bits 2.0e-4, without it 2.7e-4; 12 heads of 64 7.2 -> 7.6 us, 65536 keys 55.4 us either way).  In the
+// wide kernel, which the matrix cores bound, it is left out: causal, 8192 rows 545 us at 2.4e-4, with it 730 at 1.9e-4.
 //
 // rows kernels: sixteen query rows per workgroup, keys dealt to its four (deep: eight) wavefronts in tiles of KT;
 // each wavefront has its own ring in workgroup memory and its own maximum, sum and result, which meet at
@@ -307,6 +310,18 @@ __device__ __forceinline__ void attend_join(const AR &a, int64_t tile_id, const 
   }
 }
 
+// Two probabilities, cut off to fp16, and what that takes off them.  The rest of one that is not zero is not zero
+// either (2^-24 at least, 2^-35 of a row's largest), nor negative: an infinite value times both stays what it is.
+__device__ __forceinline__ void split_probabilities(float a, float b, uint32_t *cut, uint32_t *rest) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  const auto c = __builtin_amdgcn_cvt_pkrtz(a, b);
+  const auto r = __builtin_amdgcn_cvt_pkrtz(__builtin_fmaf((float)c[0], -1.0f, a), __builtin_fmaf((float)c[1], -1.0f, b));
+  u16x2 least;                                              // of each half: the compiler makes comparisons of it
+  asm("v_pk_min_u16 %0, %1, %2" : "=v"(least) : "v"(c), "s"(0x00010001));
+  *cut = __builtin_bit_cast(uint32_t, c);
+  *rest = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, r), least));
+}
+
 // NW: wavefronts of a workgroup.  They share its keys without the cost of a join, so that few query rows over some
 // hundred keys are best served by as many as workgroup memory holds; longer ones by smaller workgroups, of which
 // more run at once.
@@ -460,9 +475,12 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
     if constexpr (VEC) wait_loads<L>();
     else copy(vbase, a.v_s[1], a.v_width, kt, ring + TILE, std::true_type{});
     const unsigned char *W = ring + TILE;
-    V pf;
+    V pf, rest;
 #pragma unroll
-    for (int e = 0; e < VE; ++e) pf[e] = (T)p[e / 4][e % 4];
+    for (int e = 0; e < VE; e += 2) {
+      if constexpr (ES == 2) split_probabilities(p[e / 4][e % 4], p[e / 4][e % 4 + 1], (uint32_t *)&pf + e / 2, (uint32_t *)&rest + e / 2);
+      else { pf[e] = p[e / 4][e % 4]; pf[e + 1] = p[e / 4][e % 4 + 1]; }
+    }
     auto value = [&](int j) {
       if constexpr (ES == 2) {
         half4 v[2];
@@ -487,7 +505,16 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
       drop_infinite<T, TILE>(ring + TILE, lane);
     }
 #pragma unroll
-    for (int j = 0; j < NO; ++j) o[j] = mma16<T>(value(j), pf, o[j]);
+    for (int j = 0; j < NO; j += 4) {                       // four results at a time: no instruction waits for the one before
+      V v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = value(j + i);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[j + i] = mma16<T>(v[i], pf, o[j + i]);
+      if constexpr (ES == 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[j + i] = mma16<T>(v[i], rest, o[j + i]);
+    }
     if constexpr (VEC) {
       asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
       values.issue(left, lds_address(ring) + TILE);
