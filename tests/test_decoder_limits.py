@@ -1,0 +1,23 @@
+"""Sizes that the kernels of a decoder's operators cannot count or launch are refused when the DAG is built."""
+import pytest
+
+from decoder_util import build, describe
+from paper_2312_10351_amd import binding as B
+
+INT = 2 ** 31 - 1
+NORM = dict(m=4, n=8, eps=1e-5, alpha=1.0, beta=1.0, flags=B.FLAG_NORM_AFTER | B.FLAG_NORM_BEFORE)
+
+
+def refused(kind, n_inputs, dtype="f16", **fields):
+    with pytest.raises(B.OparaError) as e:
+        build(describe(kind, dtype, n_inputs, **fields))
+    return e.value.status == B.EUNSUPPORTED
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("n", [8, 7, 512, 4096])
+def test_rows_that_a_norm_counts(dtype, n):
+    """The counter of a workgroup passes the last row by up to 4096 before it stops."""
+    build(describe(B.RESIDUAL_NORM, dtype, 2, **{**NORM, "m": INT - 4096, "n": n}))
+    for m in (INT - 4095, INT):
+        assert refused(B.RESIDUAL_NORM, 2, dtype, **{**NORM, "m": m, "n": n})
