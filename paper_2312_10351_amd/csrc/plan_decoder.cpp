@@ -65,6 +65,7 @@ int plan_norm(const opara_op_desc &op, const opara_op_more &q, const void *const
   if (p.m <= 0 || p.n <= 0) return fail("bad residual norm shape", op);
   // A workgroup's row counter steps past the last row, by at most four rows of 1024 workgroups, in 32 bits.
   if (p.m > kInt - 4 * 1024) return too_large("more rows than a kernel counts", op);
+  if (p.n > (1 << 30)) return too_large("more columns than a kernel counts", op);   // the weights of both norms are one row
   if (p.batch < 0 || (p.batch > 0 && p.m % p.batch)) return fail("rows must be a multiple of the gate's rows", op);
   if (op.n_inputs < 3 && p.batch > 0) return fail("gate rows without a gate", op);
   if (!(p.eps >= 0.f)) return fail("negative eps", op);

@@ -21,3 +21,11 @@ def test_rows_that_a_norm_counts(dtype, n):
     build(describe(B.RESIDUAL_NORM, dtype, 2, **{**NORM, "m": INT - 4096, "n": n}))
     for m in (INT - 4095, INT):
         assert refused(B.RESIDUAL_NORM, 2, dtype, **{**NORM, "m": m, "n": n})
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_columns_that_a_norm_counts(dtype):
+    """The second norm's weights follow the first's: column n + j is a 32-bit number."""
+    build(describe(B.RESIDUAL_NORM, dtype, 2, **{**NORM, "n": 2 ** 30}))
+    for n in (2 ** 30 + 1, 2 ** 30 + 8, INT):
+        assert refused(B.RESIDUAL_NORM, 2, dtype, **{**NORM, "n": n})
