@@ -147,7 +147,8 @@ int plan_gated(const opara_op_desc &op, const opara_op_more &q, const void *cons
   a.relu = q.activation;
   a.alpha = 1.0f;
   a.HoWo = a.Wo = a.Cin = a.kw = 1;
-  if (p.m > kInt - 64 || p.k > kInt - 64) return too_large("more rows or columns than one launch holds", op);
+  // Kernels count K past its end in 32 bits: to the end of a tile, with one row to the end of two wavefronts' vectors.
+  if (p.m > kInt - 64 || p.k > kInt - 2048) return too_large("more rows or columns than one launch holds", op);
   auto set = [&](int kernel, int rows, int cols, int threads) {
     out->kernel = kernel;
     out->gx = (uint32_t)cdiv(p.m, rows); out->gy = (uint32_t)cdiv(p.n, cols); out->gz = 1; out->block = threads;

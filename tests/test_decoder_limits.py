@@ -29,3 +29,13 @@ def test_columns_that_a_norm_counts(dtype):
     build(describe(B.RESIDUAL_NORM, dtype, 2, **{**NORM, "n": 2 ** 30}))
     for n in (2 ** 30 + 1, 2 ** 30 + 8, INT):
         assert refused(B.RESIDUAL_NORM, 2, dtype, **{**NORM, "n": n})
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("m", [1, 3])
+def test_row_lengths_that_a_gated_block_counts(dtype, m):
+    """One row: a wavefront looks two of its vectors (2 * 512 elements in fp16) past where it is."""
+    shape = dict(m=m, n=16, weight=0x2000)
+    build(describe(B.GATED, dtype, 1, k=INT - 2048, **shape))
+    for k in (INT - 2047, INT - 1000, INT - 64, INT):
+        assert refused(B.GATED, 1, dtype, k=k, **shape)
