@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
+#include <cstdint>
 #include <cstring>
 #include "opara_internal.h"
 
@@ -341,12 +342,16 @@ int plan_attention(const opara_op_desc &op, const opara_op_more &q, const void *
 }  // namespace
 
 int plan_decoder(const opara_op_desc &op, const opara_op_more &more, const void *const *in, KernelPlan *out) {
+  int rc;
   switch (op.op_type) {
-    case OPARA_ROTARY: return plan_rotary(op, more, in, out);
-    case OPARA_RESIDUAL_NORM: return plan_norm(op, more, in, out);
-    case OPARA_GATED: return plan_gated(op, more, in, out);
-    default: return plan_attention(op, more, in, out);
+    case OPARA_ROTARY: rc = plan_rotary(op, more, in, out); break;
+    case OPARA_RESIDUAL_NORM: rc = plan_norm(op, more, in, out); break;
+    case OPARA_GATED: rc = plan_gated(op, more, in, out); break;
+    default: rc = plan_attention(op, more, in, out);
   }
+  // A launch counts the threads along an axis in 32 bits.
+  if (rc == OPARA_OK && (uint64_t)out->gx * out->block > UINT32_MAX) return too_large("more rows or columns than one launch holds", op);
+  return rc;
 }
 
 }  // namespace opara

@@ -39,3 +39,16 @@ def test_row_lengths_that_a_gated_block_counts(dtype, m):
     build(describe(B.GATED, dtype, 1, k=INT - 2048, **shape))
     for k in (INT - 2047, INT - 1000, INT - 64, INT):
         assert refused(B.GATED, 1, dtype, k=k, **shape)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_threads_that_a_launch_counts(dtype):
+    """Workgroups times threads along an axis stay below 2^32."""
+    attend = dict(n=1, heads=1, kv_heads=1, width=1, alpha=1.0)
+    build(describe(B.ATTENTION, dtype, 3, m=2 ** 27, **attend))
+    assert refused(B.ATTENTION, 3, dtype, m=2 ** 28, **attend)           # sixteen rows, 256 threads
+    gated = dict(k=1, weight=0x2000)
+    build(describe(B.GATED, dtype, 1, m=2 ** 29, n=1, **gated))
+    assert refused(B.GATED, 1, dtype, m=2 ** 30, n=1, **gated)           # 64 rows
+    build(describe(B.GATED, dtype, 1, m=1, n=2 ** 25, **gated))
+    assert refused(B.GATED, 1, dtype, m=1, n=2 ** 26, **gated)           # four columns
