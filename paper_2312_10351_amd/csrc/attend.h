@@ -364,7 +364,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
           for (int e = 0; e < VE; ++e)
             if (d + e < a.width) v[e] = q[d + e];
       }
-      qf[s] = a.negative ? -v : v;
+      qf[s] = v * (T)a.sign;
     }
   }
   const T *kbase = (const T *)a.k + z * a.k_s[0] + g * a.k_s[2], *vbase = (const T *)a.v + z * a.v_s[0] + g * a.v_s[2];
@@ -624,7 +624,7 @@ __device__ __forceinline__ void attend_wide_body(const AR &a, const Blk &b, unsi
           for (int e = 0; e < 8; ++e)
             if (d + e < a.width) v[e] = q[d + e];
       }
-      qf[x][s] = a.negative ? -v : v;
+      qf[x][s] = v * (T)a.sign;
     }
   }
   KeyStager<T, DP, KT, L, false> keys;

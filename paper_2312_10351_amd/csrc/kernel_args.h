@@ -128,7 +128,7 @@ struct AttendArgs {
   int32_t tiles, splits;
   uint32_t div_share, div_splits;
   float scale;                  // |alpha| * log2(e), above zero: exponentials are powers of two
-  int32_t negative;             // alpha < 0: the queries change sign
+  float sign;                   // of alpha, 0 for 0: the queries are multiplied by it
 };
 
 // X(name, ArgsType).  Order defines kernel ids.

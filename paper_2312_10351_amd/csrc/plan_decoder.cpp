@@ -320,9 +320,9 @@ int plan_attention(const opara_op_desc &op, const opara_op_more &q, const void *
   a.batch = (int32_t)s.batch;
   a.causal = (p.flags & OPARA_FLAG_CAUSAL) ? 1 : (p.flags & OPARA_FLAG_CAUSAL_END) ? 2 : 0;
   a.first = q.first;
-  // Above zero, so that a masked score stays -inf: with alpha 0 all visible keys count the same.
+  // Above zero, so that a masked score stays -inf: with alpha 0 the queries are zeros and all visible keys count the same.
   a.scale = std::max(std::fabs(p.alpha) * 1.44269504088896341f, FLT_MIN);
-  a.negative = p.alpha < 0.f;
+  a.sign = p.alpha < 0.f ? -1.f : p.alpha > 0.f ? 1.f : 0.f;
   a.tiles = (int32_t)pick.tiles;
   a.splits = (int32_t)pick.splits;
   if (a.splits > 1) {

@@ -68,3 +68,18 @@ def test_few_rows_are_off_by_the_rounding_of_their_result(m, n, heads, kv, width
     bound = 4.0 * D.U * 64 * LOG2 + 2.0 ** -21 + 2.0 ** -20 + 2.0 * (n / 64 + 64) * D.U + n * 2.0 ** -35
     D.within(s.result(0), want, torch.full_like(want, bound), "f16")
     s.close()
+
+
+@pytest.mark.parametrize("m, n, width", [(1, 1500, 64), (40, 300, 33), (3, 200, 256), (200, 700, 128)])
+def test_a_factor_of_zero_counts_keys_alike_whatever_their_scores(m, n, width):
+    """Products of queries and keys near fp32's largest numbers times zero are zero."""
+    g = torch.Generator().manual_seed(n)
+    q = torch.full((m, width), 1e18)
+    k = 1e18 * torch.rand(n, width, generator=g)
+    v = torch.randn(n, width, generator=g)
+    s = D.bind(lambda b, e: b.attention(*e, heads=1, width=width, alpha=0.0), [q, k, v], dtype="f32")
+    s.launch()
+    torch.cuda.synchronize()
+    want = v.double().mean(0, keepdim=True).expand(m, -1)
+    D.within(s.result(0), want, (v.abs().double().mean(0) * (n / 64 + 64) * 3 * D.U).expand(m, -1), "f32")
+    s.close()
