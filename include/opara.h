@@ -84,7 +84,7 @@ enum opara_activation {
   OPARA_ACT_SILU = 0,        /* x / (1 + exp(-x))                                          */
   OPARA_ACT_GELU = 1,        /* exact erf form                                             */
   OPARA_ACT_GELU_TANH = 2,   /* 0.5 x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3)))            */
-  OPARA_ACT_RELU = 3,
+  OPARA_ACT_RELU = 3,        /* x, 0 below zero; like the others it keeps NaN              */
   OPARA_ACT_SIGMOID = 4,
   OPARA_N_ACTIVATIONS
 };

@@ -22,7 +22,7 @@ template <typename T> __device__ __forceinline__ float gate_apply(int act, float
       const float t = 0.79788456080286536f * (x + 0.044715f * x * x * x);
       return over(x, 1.0f + ex(-2.0f * t));
     }
-    case 3: return fmaxf(x, 0.f);
+    case 3: return x < 0.f ? 0.f : x;                       // NaN stays, as in the others
     default: return over(1.0f, 1.0f + ex(-x));
   }
 }
