@@ -18,6 +18,15 @@ def _is_image(op):
         or (op.type in ("add", "relu", "gelu") and len(op.out_shape) == 3)
 
 
+def _placed(device):
+    """A GPU's number stated: "cuda" is the one that is current now."""
+    import torch
+    on = torch.device(device)
+    if on.type == "cuda" and on.index is None:
+        on = torch.device("cuda", torch.cuda.current_device())
+    return on
+
+
 def _hip():
     import torch  # noqa: F401  (makes sure the HIP runtime PyTorch uses is the one loaded)
     return C.CDLL("libamdhip64.so.7") if not hasattr(_hip, "lib") else _hip.lib
@@ -66,14 +75,14 @@ class Session:
         library id of workload operator v (absent if removed), `self.elided` the removed
         concatenations.  Outputs are still addressed by workload id."""
         self.wl = wl
-        self.device = device
-        self._index = None
+        self.device = None if device is None else str(_placed(device))
         self.dag = None
         self.execs = []
         self._workspaces = []
         self.streams = None
         self.capture_log = []
         self._fake = 0x10000
+        self._eager = None
         self._keep = []
         self.dtype_id = B.F32 if wl.dtype == "f32" else B.F16
         ve = 4 if wl.dtype == "f32" else 8
@@ -210,8 +219,7 @@ class Session:
             return self._fake_ptr(arr.nbytes)
         import torch
         if isinstance(arr, torch.Tensor):
-            on = torch.device(self.device)
-            if arr.device.type != on.type or (on.index is not None and arr.device.index != on.index) or not arr.is_contiguous():
+            if arr.device != torch.device(self.device) or not arr.is_contiguous():
                 raise ValueError(f"a device tensor of a workload must be contiguous and on {self.device}")
             return arr
         return torch.from_numpy(np.ascontiguousarray(arr)).to(self.device)
@@ -451,8 +459,8 @@ class Session:
         """Enqueue every operator in topological order on a torch stream (None: the current one of the
         session's device): no graph, and nothing waits.  The results are in `result(...)` in that stream's order."""
         import torch
-        if self._index is None:
-            self._index = torch.device(self.device).index or 0
+        if self._eager is None:
+            self._index = torch.device(self.device).index
             self._eager = B.load().opara_run_eager
         # The raw handle of the current stream: the stream object around it costs half as much as a launch.
         handle = torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream.cuda_stream
