@@ -175,6 +175,17 @@ class Session:
         self.lib_id = {v: i for i, v in enumerate(self.lib_ops)}
         self.descs = descs
         self.dag = B.opara_build_dag_more(descs, [more[v] for v in self.lib_ops], ext_ptrs)
+        self._wait_until_built()
+
+    def _wait_until_built(self):
+        """Results and scratch memory are cleared, and host tensors copied, on the stream that is current here; launches
+        and replays run on any.  Inside a capture the clearing is a part of the graph, ahead of its launches."""
+        if self.device is None:
+            return
+        import torch
+        with torch.cuda.device(self.device):
+            if not torch.cuda.is_current_stream_capturing():
+                torch.cuda.current_stream().synchronize()
 
     def _numel(self, op_id):
         op = self.wl.ops[op_id]

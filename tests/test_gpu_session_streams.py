@@ -1,0 +1,72 @@
+"""Sessions whose launches run on another stream than the one they were built on."""
+import pytest
+import torch
+
+import decoder_util as D
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+class Busy:
+    """Some tens of milliseconds of work for a stream."""
+
+    def __init__(self):
+        self.a = torch.ones(8192, 8192, dtype=torch.float16, device=DEV)
+        self.c = torch.empty_like(self.a)
+        self.on(torch.cuda.current_stream())
+        torch.cuda.synchronize()
+
+    def on(self, stream):
+        with torch.cuda.stream(stream):
+            for _ in range(60):
+                torch.mm(self.a, self.a, out=self.c)
+
+
+def attention(seed, n=6000):
+    g = torch.Generator().manual_seed(seed)
+    q, k, v = (D.normal(g, (r, 8 * 64), "f16").to(DEV) for r in (1, n, n))
+    return [q, k, v], D.attention(q, k, v, "f16", heads=8, width=64)
+
+
+def bound(tensors):
+    return D.bind(lambda b, e: b.attention(*e, heads=8, width=64), tensors)
+
+
+def test_a_session_is_ready_for_any_stream_when_it_is_built():
+    """Its results and counters are cleared on the building stream, which has other work to do first."""
+    busy, building, side = Busy(), torch.cuda.Stream(), torch.cuda.Stream()
+    for seed in range(3):
+        tensors, want = attention(seed)
+        torch.cuda.synchronize()
+        busy.on(building)
+        with torch.cuda.stream(building):
+            s = bound(tensors)
+        s.launch(side)
+        with torch.cuda.stream(side):
+            got = s.result(0).clone()
+        torch.cuda.synchronize()
+        D.within(got, *want, "f16")
+        assert torch.equal(s.result(0), got)                   # nothing cleared it afterwards
+        s.run_eager()
+        assert torch.equal(s.result(0), got)                   # the counters are as the first launch needs them
+        s.close()
+
+
+def test_a_session_built_inside_a_capture():
+    """Clearing and launch are both in the graph."""
+    tensors, want = attention(5)
+    table = [bound(tensors)]                                   # what a first use loads is loaded before
+    table[0].launch()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s = bound(tensors)
+        s.launch()
+        got = s.result(0) * 1
+    for _ in range(3):
+        got.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        D.within(got, *want, "f16")
+    s.close()
