@@ -83,6 +83,7 @@ class Session:
         self.capture_log = []
         self._fake = 0x10000
         self._eager = None
+        self._launched_on = set()           # handles of the streams that launch() was given
         self._keep = []
         self.dtype_id = B.F32 if wl.dtype == "f32" else B.F16
         ve = 4 if wl.dtype == "f32" else 8
@@ -468,18 +469,33 @@ class Session:
 
     def launch(self, stream=None):
         """Enqueue every operator in topological order on a torch stream (None: the current one of the
-        session's device): no graph, and nothing waits.  The results are in `result(...)` in that stream's order."""
+        session's device): no graph, and nothing waits.  The results are in `result(...)` in that stream's order.
+        The memory of a session that is dropped while a stream still runs its launches is handed out again only after
+        them; a graph that has captured launches needs the session as long as it is replayed."""
         import torch
         if self._eager is None:
             self._index = torch.device(self.device).index
             self._eager = B.load().opara_run_eager
         # The raw handle of the current stream: the stream object around it costs half as much as a launch.
         handle = torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream.cuda_stream
+        if handle not in self._launched_on:
+            self._use_on(torch.cuda.current_stream(self._index) if stream is None else stream)
+            self._launched_on.add(handle)
         if torch.cuda.current_device() == self._index:
             B._check(self._eager(self.dag, handle))
         else:
             with torch.cuda.device(self._index):
                 B._check(self._eager(self.dag, handle))
+
+    def _use_on(self, stream):
+        """Tells the allocator once that a stream works on the session's memory, so that it is not handed out again
+        before what the stream has then been given is done."""
+        import torch
+        if stream.device.index != self._index:
+            raise ValueError(f"a stream of {stream.device} for a session on {self.device}")
+        for t in [*self.ext_dev, *self.w_dev.values(), *self.b_dev.values(), *self.out_dev, *self.out2_dev.values(), *self._keep]:
+            if isinstance(t, torch.Tensor):
+                t.record_stream(stream)
 
     def clear_outputs(self):
         for t in self.out_dev + list(self.out2_dev.values()):

@@ -70,3 +70,37 @@ def test_a_session_built_inside_a_capture():
         torch.cuda.synchronize()
         D.within(got, *want, "f16")
     s.close()
+
+
+def test_a_dropped_sessions_memory_waits_for_its_launches():
+    """Tensors made after a session has gone do not take its memory from a stream that still works on it."""
+    busy, side = Busy(), torch.cuda.Stream()
+    for seed in range(3):
+        tensors, want = attention(seed, 60000)
+        torch.cuda.synchronize()
+        s = bound(tensors)
+        addresses = {t.data_ptr() for t in [*s.ext_dev, *s.out_dev]}
+        sizes = [t.numel() for t in s.ext_dev]
+        busy.on(side)
+        s.launch(side)
+        with torch.cuda.stream(side):
+            got = s.result(0).clone()
+        s.close()
+        del s, tensors
+        fresh = [torch.full((n,), float("nan"), dtype=torch.float16, device=DEV) for n in sizes * 2]
+        assert not addresses & {t.data_ptr() for t in fresh}
+        torch.cuda.synchronize()
+        D.within(got, *want, "f16")
+
+
+def test_streams_of_another_device_are_refused():
+    tensors, _ = attention(1)
+    s = bound(tensors)
+
+    class Elsewhere:
+        cuda_stream, device = 0x1234, torch.device("cuda", 7)
+
+    for _ in range(2):
+        with pytest.raises(ValueError):
+            s.launch(Elsewhere())
+    s.close()
