@@ -89,10 +89,22 @@ class Builder:
         return self.add(kind, xs, [(r, c)] * len(xs), (r, c), params or {}, name)
 
     # ---- the blocks of a decoder, logical [rows, heads * width]
+    def _expect(self, t, shape, what):
+        if tuple(self.shape(t)) != shape:
+            raise ValueError(f"{what}: shape {tuple(self.shape(t))}, not {shape}")
+
+    def _expect_integers(self, t, n, what):
+        if t >= 0:
+            raise ValueError(f"{what}: operators make no integers, an external tensor is needed")
+        self._expect(t, (n,), what)
+
     def rotary(self, x, heads, width, rotated=None, interleaved=False, first=0, positions=None, base=10000.0, factor=1.0,
                original=0.0, low=1.0, high=4.0, alpha=1.0, name=""):
         """Rotary positions of every head's first `rotated` columns; row r stands at first + r or at positions[r]."""
         m = self.shape(x)[0]
+        self._expect(x, (m, heads * width), "input")
+        if positions is not None:
+            self._expect_integers(positions, m, "positions")
         p = dict(heads=heads, width=width, rotated=rotated or width, interleaved=bool(interleaved), first=first, base=base,
                  factor=factor, original=original, low=low, high=high, alpha=alpha)
         extra = [] if positions is None else [positions]
@@ -105,10 +117,15 @@ class Builder:
         m, n = self.shape(x)
         inputs, shapes = [x], [(m, n)]
         if residual is not None:
+            self._expect(residual, (m, n), "residual")
             inputs.append(residual)
             shapes.append((m, n))
         if gate is not None:
             assert residual is not None, "a gate goes with a residual"
+            rows = self.shape(gate)[0]
+            self._expect(gate, (rows, n), "gate")
+            if rows < 1 or m % rows:
+                raise ValueError(f"gate: {rows} rows for {m}")
             inputs.append(gate)
             shapes.append(tuple(self.shape(gate)))
         p = dict(rms=bool(rms), after=bool(after), before=bool(before), alpha=alpha, beta=beta, eps=eps, gates=shapes[2][0] if gate is not None else 0,
@@ -117,13 +134,23 @@ class Builder:
 
     def gated(self, x, m, k, n, activation="silu", name=""):
         """activation(x . w[:, :n]) * (x . w[:, n:])"""
+        shape = self.shape(x)                      # its first m rows, or all of it in another shape
+        if int(np.prod(shape)) != m * k and (len(shape) != 2 or shape[0] < m or shape[1] != k):
+            raise ValueError(f"input: {m} rows of {k} are read from shape {shape}")
         return self.add("gated", [x], [(m, k)], (m, n), dict(m=m, k=k, n=n, activation=activation), name)
 
     def attention(self, q, k, v, heads, width, kv_heads=None, v_width=None, batch=1, lengths=None, causal=None, first=0, alpha=None, name=""):
         """Attention of `batch` sequences' query rows to key rows of another number; causal: None, "start" (row i sees
         i + first + 1 keys) or "end" (the last row sees all of its sequence)."""
         kv_heads, v_width = kv_heads or heads, v_width or width
+        if batch < 1 or self.shape(q)[0] % batch or self.shape(k)[0] % batch:
+            raise ValueError(f"{self.shape(q)[0]} query and {self.shape(k)[0]} key rows are not {batch} sequences of one length")
         m, n = self.shape(q)[0] // batch, self.shape(k)[0] // batch
+        for t, shape, what in ((q, (batch * m, heads * width), "queries"), (k, (batch * n, kv_heads * width), "keys"),
+                               (v, (batch * n, kv_heads * v_width), "values")):
+            self._expect(t, shape, what)
+        if lengths is not None:
+            self._expect_integers(lengths, batch, "lengths")
         p = dict(heads=heads, kv_heads=kv_heads, width=width, v_width=v_width, batch=batch, m=m, n=n, causal=causal, first=first,
                  alpha=1.0 / float(np.sqrt(width)) if alpha is None else alpha)
         inputs = [q, k, v] + ([] if lengths is None else [lengths])
