@@ -194,24 +194,24 @@ class Session:
 
     # ---- device memory (PyTorch) or fake addresses when there is no device
     def _check_tensors(self):
-        """Positions and lengths are int32; tensors that are used in place have the type and size that the operators read."""
-        import torch
+        """Positions and lengths are int32; arrays and tensors have the type and size that the operators read (biases on
+        the host any type: they are converted)."""
         wl = self.wl
-        own = {"f32": torch.float32, "f16": torch.float16}[wl.dtype]
+        own = {"f32": "float32", "f16": "float16"}[wl.dtype]
 
         def check(t, numel, dtype, what):
-            if isinstance(t, torch.Tensor) and (t.dtype != dtype or t.numel() < numel):
-                raise ValueError(f"{what}: {numel} elements of {dtype} are read, the tensor has {t.numel()} of {t.dtype}")
+            host = isinstance(t, np.ndarray)
+            size, kind = t.size if host else t.numel(), str(t.dtype).split(".")[-1]
+            if size < numel or kind != dtype and not (host and what.startswith("bias")):
+                raise ValueError(f"{what}: {numel} elements of {dtype} are read, there are {size} of {kind}")
 
         for op in wl.ops:
             whole = {"rotary": 1, "attention": 3}.get(op.type)
             for i, (u, shape) in enumerate(zip(op.inputs, op.in_shapes)):
                 if u >= 0:
                     continue
-                t, what = wl.ext_inputs[-u - 1], f"input {i} of {op.name}"
-                if i == whole and str(t.dtype).split(".")[-1] != "int32":
-                    raise ValueError(f"{what}: positions and lengths are int32, not {t.dtype}")
-                check(t, int(np.prod(shape)) * (wl.batch if _is_image(op) else 1), torch.int32 if i == whole else own, what)
+                check(wl.ext_inputs[-u - 1], int(np.prod(shape)) * (wl.batch if _is_image(op) else 1), "int32" if i == whole else own,
+                      f"input {i} of {op.name}")
             if op.id not in wl.weights:
                 continue
             q, w = op.params, wl.weights[op.id]
@@ -224,7 +224,7 @@ class Session:
             else:
                 continue
             check(w["w"], n_w, own, f"weight of {op.name}")
-            check(w["b"], n_b, torch.float32, f"bias of {op.name}")
+            check(w["b"], n_b, "float32", f"bias of {op.name}")
 
     def _upload(self, arr):
         if self.device is None:
