@@ -235,30 +235,41 @@ int attend_shape(const opara_op_desc &op, const opara_op_more &q, AttendShape *s
 // a cache (`alone`) or, all of them more than kAttendCached, come from memory (`far`), and in a full launch (`busy`);
 // microseconds of the launch and everything else outside the keys (`fixed`), of every further 256 workgroups
 // (`each`), of a join (`join`), of every workgroup that a tile is joined from (`part`) and of every 256 that leave a
-// record (`records`).  Fitted to about 1000 launches per type and width (1..2048 rows of 1..32 key heads,
-// 128..65536 keys, 1..256 splits) within 5 to 17 %; the form and split it picks are 2 % slower than the best in the mean.
+// record (`records`).  Fitted to 600 to 1000 launches per type and width (1..2048 rows of 1..32 key heads,
+// 60..65536 keys, 1..256 splits) within 5 to 21 %, fp16 of width 256 apart, whose row is an estimate.  What they pick
+// for keys that are loaded directly is 1 to 3 % slower than the best in the mean and 32 % at worst (one row of 12 heads of
+// 256, 65536 keys), for unaligned keys, which go through registers, 1 to 5 % and 45 %; these priced as the others
+// (20 times too fast) were 6 to 42 % slower than the best, up to 3.7 times (one row of 32 heads over 8 of 101,
+// 16384 keys: 258 us, now 69).
 // The deep forms (eight wavefronts) against four: 12 heads of 64, 1500 keys, one row 8.0 -> 7.2 us, one key head of 64,
 // 2048 rows, 4096 keys 16.8 -> 12.3; where many workgroups run at once the small ones are the faster, 12 heads of 64,
 // 1024 rows, 512 keys 11.9 and 9.4.
 struct AttendForm {
-  int kernel, any, rows, key_tile, threads;                 // any: for unaligned keys, -1 none
+  int kernel, rows, key_tile, threads;
   double alone, far, busy, fixed, each, join, part, records;
 };
 constexpr double kAttendCached = 85e6;
 const AttendForm kAttendF16[3][3] = {
-    {{K_attend_f16_rows64, K_attend_f16_any64, 16, 128, 256, 3.7, 6.7, 3.1, 3.7, 0.39, 2.4, 0.080, 1.7},
-     {K_attend_f16_deep64, -1, 16, 256, 512, 2.4, 6.6, 3.1, 4.0, 0.79, 3.7, 0.027, 2.9},
-     {K_attend_f16_wide64, -1, 128, 64, 256, 13.7, 14.0, 10.4, 4.5, 0.79, 2.9, 0.440, 1.9}},
-    {{K_attend_f16_rows128, K_attend_f16_any128, 16, 128, 256, 4.9, 10.9, 6.5, 4.7, 0.95, 2.3, 0.095, 1.9},
-     {K_attend_f16_deep128, -1, 16, 256, 512, 4.9, 10.6, 7.0, 4.4, 1.80, 3.6, 0.038, 4.5},
-     {K_attend_f16_wide128, -1, 128, 64, 256, 21.2, 21.2, 16.6, 5.8, 1.78, 3.1, 0.804, 3.7}},
-    {{K_attend_f16_rows256, K_attend_f16_any256, 16, 128, 256, 16.0, 16.0, 22.0, 6.0, 2.50, 2.5, 0.150, 3.0}}};
+    {{K_attend_f16_rows64, 16, 128, 256, 3.7, 6.7, 3.1, 3.7, 0.39, 2.4, 0.080, 1.7},
+     {K_attend_f16_deep64, 16, 256, 512, 2.4, 6.6, 3.1, 4.0, 0.79, 3.7, 0.027, 2.9},
+     {K_attend_f16_wide64, 128, 64, 256, 13.7, 14.0, 10.4, 4.5, 0.79, 2.9, 0.440, 1.9}},
+    {{K_attend_f16_rows128, 16, 128, 256, 4.9, 10.9, 6.5, 4.7, 0.95, 2.3, 0.095, 1.9},
+     {K_attend_f16_deep128, 16, 256, 512, 4.9, 10.6, 7.0, 4.4, 1.80, 3.6, 0.038, 4.5},
+     {K_attend_f16_wide128, 128, 64, 256, 21.2, 21.2, 16.6, 5.8, 1.78, 3.1, 0.804, 3.7}},
+    {{K_attend_f16_rows256, 16, 128, 256, 16.0, 16.0, 22.0, 6.0, 2.50, 2.5, 0.150, 3.0}}};
 const AttendForm kAttendF32[3][3] = {
-    {{K_attend_f32_rows64, K_attend_f32_any64, 16, 64, 256, 12.3, 13.4, 10.6, 4.1, 0.48, 2.4, 0.082, 1.2},
-     {K_attend_f32_deep64, -1, 16, 128, 512, 9.4, 11.0, 10.5, 4.6, 1.22, 3.7, 0.031, 1.7}},
-    {{K_attend_f32_rows128, K_attend_f32_any128, 16, 64, 256, 20.9, 21.1, 21.8, 5.0, 1.17, 2.7, 0.093, 1.2},
-     {K_attend_f32_deep128, -1, 16, 128, 512, 16.9, 19.5, 21.5, 5.5, 3.27, 3.7, 0.052, 2.8}},
-    {{K_attend_f32_rows256, K_attend_f32_any256, 16, 64, 256, 43.3, 43.3, 50.6, 7.6, 4.97, 1.9, 0.146, 1.0}}};
+    {{K_attend_f32_rows64, 16, 64, 256, 12.3, 13.4, 10.6, 4.1, 0.48, 2.4, 0.082, 1.2},
+     {K_attend_f32_deep64, 16, 128, 512, 9.4, 11.0, 10.5, 4.6, 1.22, 3.7, 0.031, 1.7}},
+    {{K_attend_f32_rows128, 16, 64, 256, 20.9, 21.1, 21.8, 5.0, 1.17, 2.7, 0.093, 1.2},
+     {K_attend_f32_deep128, 16, 128, 512, 16.9, 19.5, 21.5, 5.5, 3.27, 3.7, 0.052, 2.8}},
+    {{K_attend_f32_rows256, 16, 64, 256, 43.3, 43.3, 50.6, 7.6, 4.97, 1.9, 0.146, 1.0}}};
+const AttendForm kAttendAny[2][3] = {                       // unaligned keys; f32, f16
+    {{K_attend_f32_any64, 16, 64, 256, 60.2, 95.8, 26.9, 2.4, 0.0, 2.0, 0.093, 2.0},
+     {K_attend_f32_any128, 16, 64, 256, 119.0, 181.0, 89.8, 1.9, 0.0, 3.1, 0.138, 1.1},
+     {K_attend_f32_any256, 16, 64, 256, 251.0, 341.0, 299.0, 2.0, 0.0, 4.2, 0.190, 0.0}},
+    {{K_attend_f16_any64, 16, 128, 256, 51.4, 71.3, 17.8, 2.0, 0.0, 1.0, 0.106, 2.8},
+     {K_attend_f16_any128, 16, 128, 256, 106.0, 159.0, 71.6, 2.0, 0.0, 3.2, 0.141, 0.4},
+     {K_attend_f16_any256, 16, 128, 256, 168.0, 217.0, 196.0, 3.1, 0.0, 3.9, 0.203, 0.0}}};
 
 struct AttendPick { const AttendForm *form; int64_t tiles, splits, counter_bytes, scratch; };
 
@@ -266,13 +277,12 @@ struct AttendPick { const AttendForm *form; int64_t tiles, splits, counter_bytes
 AttendPick attend_pick(const opara_op_desc &op, const AttendShape &s, bool vec, uint64_t room) {
   const bool f16 = op.dtype == OPARA_F16;
   const int size = s.dp == 64 ? 0 : s.dp == 128 ? 1 : 2;
-  const AttendForm *forms = f16 ? kAttendF16[size] : kAttendF32[size];
+  const AttendForm *forms = !vec ? &kAttendAny[f16][size] : f16 ? kAttendF16[size] : kAttendF32[size];
   const double bytes = s.batch * s.kv_heads * s.keys * (s.width + s.v_width) * (f16 ? 2 : 4);
   AttendPick best{};
   double least = 0.0;
-  for (int i = 0; i < 3 && forms[i].rows; ++i) {
+  for (int i = 0; i < (vec ? 3 : 1) && forms[i].rows; ++i) {
     const AttendForm &f = forms[i];
-    if (!vec && f.any < 0) continue;
     const int64_t tiles = cdiv((int64_t)op.params.m * s.share, f.rows), work = tiles * s.kv_heads * s.batch;
     for (int64_t n = 1; n <= kAttendMaxSplits; n = n < 4 ? n + 1 : n + n / 2) {
       if (n > 1 && n * f.key_tile > s.keys) break;           // two tiles for every wavefront
@@ -331,10 +341,10 @@ int plan_attention(const opara_op_desc &op, const opara_op_more &q, const void *
   }
   a.div_share = div_magic(s.share);
   a.div_splits = div_magic(a.splits);
-  out->kernel = vec ? pick.form->kernel : pick.form->any;
+  out->kernel = pick.form->kernel;
   const int64_t gx = pick.tiles * pick.splits;
   if (gx * s.kv_heads * s.batch > kInt) return too_large("more rows than one launch holds", op);
-  out->gx = (uint32_t)gx; out->gy = (uint32_t)s.kv_heads; out->gz = (uint32_t)s.batch; out->block = (uint32_t)(vec ? pick.form->threads : 256);
+  out->gx = (uint32_t)gx; out->gy = (uint32_t)s.kv_heads; out->gz = (uint32_t)s.batch; out->block = (uint32_t)pick.form->threads;
   out->args.attend = a;
   return OPARA_OK;
 }
