@@ -470,8 +470,9 @@ class Session:
     def launch(self, stream=None):
         """Enqueue every operator in topological order on a torch stream (None: the current one of the
         session's device): no graph, and nothing waits.  The results are in `result(...)` in that stream's order.
-        The memory of a session that is dropped while a stream still runs its launches is handed out again only after
-        them; a graph that has captured launches needs the session as long as it is replayed."""
+        The memory of a session that is dropped while one of torch's streams still runs its launches is handed out again
+        only after them.  Streams made elsewhere (ExternalStream) and graphs that have captured launches need the session
+        until they are done.  All launches share the results and scratch memory: they must not overlap."""
         import torch
         if self._eager is None:
             self._index = torch.device(self.device).index
@@ -489,10 +490,13 @@ class Session:
 
     def _use_on(self, stream):
         """Tells the allocator once that a stream works on the session's memory, so that it is not handed out again
-        before what the stream has then been given is done."""
+        before what the stream has then been given is done.  The allocator asks the stream when the memory is freed: one
+        that torch did not make, whose number is its handle, may have been destroyed by then."""
         import torch
         if stream.device.index != self._index:
             raise ValueError(f"a stream of {stream.device} for a session on {self.device}")
+        if stream.cuda_stream and stream.stream_id == stream.cuda_stream:
+            return
         for t in [*self.ext_dev, *self.w_dev.values(), *self.b_dev.values(), *self.out_dev, *self.out2_dev.values(), *self._keep]:
             if isinstance(t, torch.Tensor):
                 t.record_stream(stream)

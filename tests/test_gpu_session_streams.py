@@ -104,3 +104,26 @@ def test_streams_of_another_device_are_refused():
         with pytest.raises(ValueError):
             s.launch(Elsewhere())
     s.close()
+
+
+def test_streams_that_end_before_the_session():
+    """The allocator is not told of streams that their owner destroys, the session's own among them."""
+    tensors, want = attention(2)
+    torch.cuda.synchronize()
+    for foreign in (lambda s: s.make_streams(1).torch_streams[0], lambda s: torch.cuda.ExternalStream(s.make_streams(2).handles[1])):
+        s = bound(tensors)
+        stream = foreign(s)
+        assert stream.stream_id == stream.cuda_stream != 0
+        s.launch(stream)
+        with torch.cuda.stream(stream):                        # as the current stream it is another object
+            assert torch.cuda.current_stream().stream_id == stream.stream_id
+            s.launch()
+        torch.cuda.synchronize()
+        D.within(s.result(0), *want, "f16")
+        s.close()
+        del s, stream
+        fresh = [torch.empty(n, device=DEV) for n in (64, 1 << 20, 1 << 24)]
+        del fresh
+        torch.cuda.empty_cache()
+    pool, default = torch.cuda.Stream(), torch.cuda.default_stream()
+    assert pool.stream_id != pool.cuda_stream and default.stream_id == 0
