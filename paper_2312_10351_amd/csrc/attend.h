@@ -4,7 +4,7 @@
 // The query heads that share a key and value head are further query rows of it (row = i * share +
 // head in the share), so that the keys are read once for all of them.  Scores are formed
 // transposed, S^T = K Q^T: a lane then holds one query row and a few keys of it, the maximum and sum
-// of a row need two shuffles per tile, and its probabilities already lie where the second product wants them,
+// of a row need two lane swaps per tile, and its probabilities already lie where the second product wants them,
 // O^T += V^T P^T (both operands number the keys of a step alike, in whatever order).
 // Statistics and sums are fp32.  The matrix cores take probabilities of the element type, in fp16 rounded by relative
 // 2^-11, while their sum is taken before that.  They are formed 2^kAttendLift times too large, a factor that the sum
@@ -21,9 +21,9 @@
 // workgroups: each leaves (maximum, sum, result) in scratch memory and the last to arrive joins them in
 // a fixed order, so the result does not depend on who that is.
 // What bounds them: few rows over many keys the keys' bytes (fp16, 32 heads over 8 of 128, 65536 keys, one row:
-// 54.6 us, 4.9 TB/s, a large copy runs at 4.9); few rows over few keys latencies, launch, first loads and
-// join (12 heads of 64, 1500 keys: 7.2 us, of which an empty launch takes 2.2); many rows in fp32 the matrix
-// cores (32 heads over 8 of 128, causal, 2048 rows: 322 us, 107 TFLOP/s, a large matrix product reaches 154).
+// 55 us, 4.9 TB/s, a large copy runs at 4.9); few rows over few keys latencies, launch, first loads and
+// join (12 heads of 64, 1500 keys: 7.6 us, of which an empty launch takes 2.2); many rows in fp32 the matrix
+// cores (32 heads over 8 of 128, causal, 2048 rows: 320 to 329 us, 105 to 107 TFLOP/s, a large matrix product reaches 154).
 // Lanes hold whole rows of scores in registers: one wavefront works on a tile for about 1 us, 0.4 of it matrix
 // instructions, so that several per SIMD are wanted.
 
@@ -581,8 +581,8 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
 // a width of 128; exponentials take a quarter of the rate) and 16 KB of fragment reads each for keys and values; two
 // wavefronts per SIMD overlap the three, the one at a product first (s_setprio).  16 x 16 matrix instructions:
 // with 32 x 32 ones, which need half as many reductions, the same kernel measured 9 % slower.
-// Measured, fp16, 32 heads over 8 of 128, 8192 rows (us): causal 545 (1009 TFLOP/s), all keys 1031 (1066; a
-// large matrix product reaches 1350); 16 heads of 64, 4096 rows 88 (779).  Matrix cores busy 49 % of the
+// Measured, fp16, 32 heads over 8 of 128, 8192 rows (us): causal 543 among other work (1010 TFLOP/s), 568 to 575 launched
+// back to back, all keys 1046 (1051; a large matrix product reaches 1350); 16 heads of 64, 4096 rows 88 (779).  Matrix cores busy 49 % of the
 // compute units' cycles (causal), 256 vector instructions for 64 matrix instructions of 16 cycles.
 constexpr int lds_attend_wide(int dp) { return 4 * 64 * dp * 2; }
 

@@ -121,7 +121,8 @@ struct AttendArgs {
   void *y;
   const int32_t *lengths;       // [batch] or null
   uint32_t *counters;           // [batch * kv_heads * tiles], zero between launches (splits > 1)
-  float *partials;              // [batch * kv_heads * tiles * splits][16 * padded width + 32]
+  float *partials;              // [batch * kv_heads * tiles * splits] records: results, maxima and sums of a tile's rows,
+                                // rows * (padded width + 2) numbers (rows: 16, in the wide kernels 128)
   int64_t q_s[3], k_s[3], v_s[3], y_s[3];   // elements between sequences, rows, heads
   int32_t m, n, share, width, v_width;      // share: query heads per key head
   int32_t batch, causal, first; // causal: 0 no, 1 from `first`, 2 to the sequence's end

@@ -110,7 +110,9 @@ int plan_norm(const opara_op_desc &op, const opara_op_more &q, const void *const
 // The forms of the gated block that are fed through workgroup memory, and what one workgroup costs in
 // microseconds, in fp32 and in fp16: a 128-byte step of K with a compute unit to itself (`alone`) and in a full
 // launch (`busy`), and everything outside the K walk (`fixed`).  Fitted to 115 products of each type (1..2048 rows,
-// 256..4096 -> 512..12288, weights in no cache) within 12 %; the form it picks is 2 % slower than the best in the mean.
+// 256..4096 -> 512..12288, weights in no cache) within 12 %; the form it picks is 2 % slower than the best in the mean
+// and 25 % at worst, most of all at 64 to 200 rows of the largest (192 rows of 4096 -> 12288 in fp32: 64 x 32 tiles
+// 375 us, 32 x 32 ones 300; 128 rows in fp16: 128 x 64 tiles 68, 64 x 32 ones 58).
 struct GatedCost { double alone, busy, fixed; };
 struct GatedForm { int ids[2], rows, cols, threads; GatedCost cost[2]; };            // f32, f16
 const GatedForm kGatedForms[] = {
@@ -236,14 +238,15 @@ int attend_shape(const opara_op_desc &op, const opara_op_more &q, AttendShape *s
 // microseconds of the launch and everything else outside the keys (`fixed`), of every further 256 workgroups
 // (`each`), of a join (`join`), of every workgroup that a tile is joined from (`part`) and of every 256 that leave a
 // record (`records`).  Fitted to 600 to 1000 launches per type and width (1..2048 rows of 1..32 key heads,
-// 60..65536 keys, 1..256 splits) within 5 to 21 %, fp16 of width 256 apart, whose row is an estimate.  What they pick
+// 60..65536 keys, 1..256 splits) within 5 to 21 %, fp16 of width 256 apart, whose row is an estimate; the fp16 rows forms
+// before they had a second product, which costs up to 7 %.  What they pick
 // for keys that are loaded directly is 1 to 3 % slower than the best in the mean and 32 % at worst (one row of 12 heads of
 // 256, 65536 keys), for unaligned keys, which go through registers, 1 to 5 % and 45 %; these priced as the others
-// (20 times too fast) were 6 to 42 % slower than the best, up to 3.7 times (one row of 32 heads over 8 of 101,
+// (5 to 22 times too fast) were 6 to 42 % slower than the best, up to 3.7 times (one row of 32 heads over 8 of 101,
 // 16384 keys: 258 us, now 69).
-// The deep forms (eight wavefronts) against four: 12 heads of 64, 1500 keys, one row 8.0 -> 7.2 us, one key head of 64,
-// 2048 rows, 4096 keys 16.8 -> 12.3; where many workgroups run at once the small ones are the faster, 12 heads of 64,
-// 1024 rows, 512 keys 11.9 and 9.4.
+// The deep forms (eight wavefronts) against four: 12 heads of 64, 1500 keys, one row 8.0 -> 7.6 us, one key head of 64,
+// 2048 rows, 4096 keys 17.8 -> 14.2; where many workgroups run at once the small ones are the faster, 12 heads of 64,
+// 1024 rows, 512 keys 11.9 and 9.3.
 struct AttendForm {
   int kernel, rows, key_tile, threads;
   double alone, far, busy, fixed, each, join, part, records;

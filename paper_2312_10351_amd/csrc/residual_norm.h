@@ -8,8 +8,8 @@
 // the row itself).  The statistics are taken over the centred values (two passes over registers), in fp32, and
 // y is computed from s as it is before it is rounded.  A row is addressed through a buffer of its length: lanes behind
 // it read zeros and write nothing, without a branch around any load.
-// Measured (us): fp16, 4096 x 4096, two norms and a gate per channel 27.3 (134 MB, 4.9 TB/s; a large copy runs at 4.9),
-// 64 x 4096 5.5, one row of 768 3.7 (an empty launch: 2.2); fp32 1000 x 1027 with a gate per element 7.6.
+// Measured (us): fp16, 4096 x 4096, two norms and a gate per channel 28 (134 MB, 4.8 TB/s; a large copy runs at 4.9),
+// 64 x 4096 4.2, one row of 768 3.0 (an empty launch: 2.2); fp32 1000 x 1027 with a gate per element 7.9.
 
 // W elements of a row from column col on: 16 bytes of T, or one element where the rows are not made of
 // aligned 16-byte pieces.

@@ -10,8 +10,8 @@
 // `heads_each` heads, four loads in flight; adjacent threads hold adjacent columns.  Chunks are read at
 // element alignment, so odd widths and strides take the same path; a chunk that is not whole
 // goes element by element.
-// Measured (us): fp16, 32 heads of 128, one row 4.0 (an empty launch: 2.2), 77 rows 5.3, 4096 rows 12.8 (67 MB, in part
-// from caches), 16384 rows 62 (268 MB, 4.3 TB/s; a large copy runs at 4.9); fp32, 4096 rows 32 (134 MB, 4.2 TB/s).
+// Measured (us): fp16, 32 heads of 128, one row 3.3 (an empty launch: 2.2), 77 rows 3.5, 4096 rows 14.8 (67 MB),
+// 16384 rows 62 (268 MB, 4.3 TB/s; a large copy runs at 4.9); fp32, 4096 rows 32 (134 MB, 4.2 TB/s).
 
 // cos and sin of a phase in units of 2^-64 turns.
 template <typename T> __device__ __forceinline__ void turn_of(uint64_t phase, float &c, float &s) {

@@ -19,7 +19,7 @@ def workgroups(dtype, width, m, n, heads, kv):
 @pytest.mark.parametrize("odd, even", [(37, 40), (101, 104), (201, 208)])
 @pytest.mark.parametrize("m, n, heads, kv", [(1, 65536, 32, 8), (1, 16384, 32, 8), (1, 16384, 12, 12), (8, 16384, 12, 12)])
 def test_keys_that_go_through_registers_are_shared_out_further(dtype, odd, even, m, n, heads, kv):
-    """One workgroup walks them 5 to 30 times slower than keys that are loaded directly, so that more of them pay; two
+    """One workgroup walks them 5 to 22 times slower than keys that are loaded directly, so that more of them pay; two
     (of the widest: one) fit on each of 256 compute units."""
     kernel, groups = workgroups(dtype, odd, m, n, heads, kv)
     assert kernel.startswith(f"attend_{dtype}_any")
