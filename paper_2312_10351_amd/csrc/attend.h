@@ -13,7 +13,7 @@
 // What the rounding takes off a probability is an fp16 number too (but for 2^-20 of the probability), and a second
 // product adds it where bytes and latencies are the bound, in the rows kernels: a result is then off by its own rounding alone (1500 keys, root mean square
 // against 64 bits 2.0e-4, without it 2.7e-4; 12 heads of 64 7.2 -> 7.6 us, 65536 keys 55.4 us either way).  In the
-// wide kernel, which the matrix cores bound, it is left out: causal, 8192 rows 545 us at 2.4e-4, with it 730 at 1.9e-4.
+// wide kernel, which the matrix cores bound, it is left out: causal, 8192 rows 543 us at 2.5e-4, with it 730 at 1.9e-4.
 //
 // rows kernels: sixteen query rows per workgroup, keys dealt to its four (deep: eight) wavefronts in tiles of KT;
 // each wavefront has its own ring in workgroup memory and its own maximum, sum and result, which meet at
