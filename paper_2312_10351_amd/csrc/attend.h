@@ -31,8 +31,9 @@ constexpr int attend_ring_bytes(int dp) { return 2 * 64 * dp; }      // of one w
 constexpr int lds_attend_rows(int dp, int waves) { return waves * attend_ring_bytes(dp); }
 
 // A result is scaled down only when its row's maximum has grown by more than 2^kAttendSlack.  Together the two stay below
-// fp16's largest power of two, 2^15.  A slack of 8 leaves 7 for the lift; for scores of standard deviation 1 (causal,
-// 8192 rows) it costs the same, of 8 it takes 525 us against 535.
+// fp16's largest power of two, 2^15.  In fp32 there is no lift: values near its largest would leave its range.  A slack of
+// 8 leaves 7 for the lift; for scores of standard deviation 1 (causal, 8192 rows) it costs the same, of 8 it takes 525 us
+// against 535.
 constexpr float kAttendSlack = 4.f, kAttendLift = 11.f;
 
 // A row's 16-byte chunk c lies in slot c ^ attend_slot(row), so that what one fragment read takes at a time lies in
@@ -453,7 +454,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
     for (int i = 0; i < NQ; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) most = fmaxf(most, p[i][e]);
-    most = row_max(most) * a.scale - kAttendLift;           // a positive factor
+    most = row_max(most) * a.scale - (ES == 2 ? kAttendLift : 0.f);      // a positive factor
     if (__any(most > top + kAttendSlack)) {
       const float now = fmaxf(most, top), shrink = __builtin_amdgcn_exp2f(top - (now == -INFINITY ? 0.f : now));
       top = now;

@@ -83,3 +83,17 @@ def test_a_factor_of_zero_counts_keys_alike_whatever_their_scores(m, n, width):
     want = v.double().mean(0, keepdim=True).expand(m, -1)
     D.within(s.result(0), want, (v.abs().double().mean(0) * (n / 64 + 64) * 3 * D.U).expand(m, -1), "f32")
     s.close()
+
+
+@pytest.mark.parametrize("width", [64, 37, 128, 200])
+@pytest.mark.parametrize("m, n", [(1, 1), (1, 3), (40, 2)])
+def test_large_values_stay_in_fp32s_range(m, n, width):
+    """Results are sums of weights of at most one times values until they are divided by the weights' sum."""
+    g = torch.Generator().manual_seed(n)
+    q, k = torch.randn(m, width, generator=g), torch.randn(n, width, generator=g)
+    v = 1e38 * (torch.rand(n, width, generator=g) * 2 - 1)
+    s = D.bind(lambda b, e: b.attention(*e, heads=1, width=width), [q, k, v], dtype="f32")
+    s.launch()
+    torch.cuda.synchronize()
+    D.within(s.result(0), *D.attention(q, k, v, "f32", width=width), "f32")
+    s.close()
