@@ -181,7 +181,7 @@ class Session:
     def _wait_until_built(self):
         """Results and scratch memory are cleared, and host tensors copied, on the stream that is current here; launches
         and replays run on any.  Inside a capture the clearing is a part of the graph, ahead of its launches."""
-        if self.device is None:
+        if self.device is None or not self.device.startswith("cuda"):
             return
         import torch
         with torch.cuda.device(self.device):
