@@ -16,7 +16,8 @@ def test_rotary(b):
     for heads, width in ((1, 64), (2, 32), (4, 64)):
         with pytest.raises(ValueError):
             b.rotary(x, heads, width)
-    for positions in (b.ext((5,)), b.ext((7,)), b.ext((6, 1)), b.gemm(x, 6, 128, 1)):
+    b.rotary(b.ext((6, 2, 64)), 2, 64, positions=b.ext((6, 1)))      # heads as an axis
+    for positions in (b.ext((5,)), b.ext((7,)), b.ext((6, 2)), b.gemm(x, 6, 128, 1)):
         with pytest.raises(ValueError):
             b.rotary(x, 2, 64, positions=positions)
 
@@ -49,6 +50,9 @@ def test_attention(b):
     ok = dict(heads=4, width=16, kv_heads=2, v_width=8)
     b.attention(q, k, v, **ok)
     b.attention(q, k, v, **ok, batch=2, lengths=b.ext((2,)))
+    b.attention(b.ext((6, 4, 16)), b.ext((10, 2, 16)), b.ext((10, 2, 8)), **ok)
+    with pytest.raises(ValueError):                            # sequences as an axis of their own
+        b.attention(b.ext((2, 3, 64)), b.ext((2, 5, 32)), b.ext((2, 5, 16)), **ok, batch=2)
     for bad in (dict(batch=4), dict(batch=5), dict(batch=0), dict(heads=2), dict(width=8), dict(v_width=16), dict(kv_heads=1)):
         with pytest.raises(ValueError):
             b.attention(q, k, v, **{**ok, **bad})

@@ -90,13 +90,16 @@ class Builder:
 
     # ---- the blocks of a decoder, logical [rows, heads * width]
     def _expect(self, t, shape, what):
-        if tuple(self.shape(t)) != shape:
-            raise ValueError(f"{what}: shape {tuple(self.shape(t))}, not {shape}")
+        """Rows and columns of t, which may have further axes in place of its columns."""
+        have = tuple(self.shape(t))
+        if (have[0], int(np.prod(have[1:]))) != shape:
+            raise ValueError(f"{what}: shape {have}, not {shape}")
 
     def _expect_integers(self, t, n, what):
         if t >= 0:
             raise ValueError(f"{what}: operators make no integers, an external tensor is needed")
-        self._expect(t, (n,), what)
+        if int(np.prod(self.shape(t))) != n:
+            raise ValueError(f"{what}: shape {tuple(self.shape(t))}, not {(n,)}")
 
     def rotary(self, x, heads, width, rotated=None, interleaved=False, first=0, positions=None, base=10000.0, factor=1.0,
                original=0.0, low=1.0, high=4.0, alpha=1.0, name=""):
@@ -134,8 +137,8 @@ class Builder:
 
     def gated(self, x, m, k, n, activation="silu", name=""):
         """activation(x . w[:, :n]) * (x . w[:, n:])"""
-        shape = self.shape(x)                      # its first m rows, or all of it in another shape
-        if int(np.prod(shape)) != m * k and (len(shape) != 2 or shape[0] < m or shape[1] != k):
+        shape = tuple(self.shape(x))               # its first m rows, or all of it in another shape
+        if int(np.prod(shape)) != m * k and (shape[0] < m or int(np.prod(shape[1:])) != k):
             raise ValueError(f"input: {m} rows of {k} are read from shape {shape}")
         return self.add("gated", [x], [(m, k)], (m, n), dict(m=m, k=k, n=n, activation=activation), name)
 
