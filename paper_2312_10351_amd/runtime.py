@@ -10,6 +10,7 @@ import ctypes as C
 import numpy as np
 from . import binding as B
 
+_ROW_TYPES = ("rotary", "residual_norm", "gated", "attention")
 _IMAGE_TYPES = ("conv2d", "maxpool", "avgpool", "gavgpool")
 
 
@@ -210,8 +211,10 @@ class Session:
             for i, (u, shape) in enumerate(zip(op.inputs, op.in_shapes)):
                 if u >= 0:
                     continue
-                check(wl.ext_inputs[-u - 1], int(np.prod(shape)) * (wl.batch if _is_image(op) else 1), "int32" if i == whole else own,
-                      f"input {i} of {op.name}")
+                t, what = wl.ext_inputs[-u - 1], f"input {i} of {op.name}"
+                check(t, int(np.prod(shape)) * (wl.batch if _is_image(op) else 1), "int32" if i == whole else own, what)
+                if op.type in _ROW_TYPES and isinstance(t, np.ndarray) and t.ndim >= 3 and t.shape[-3] > 1 and t.shape[-2] * t.shape[-1] > 1:
+                    raise ValueError(f"{what}: host arrays of three axes are images, stored with the channels last; rows have two")
             if op.id not in wl.weights:
                 continue
             q, w = op.params, wl.weights[op.id]

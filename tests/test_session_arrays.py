@@ -1,6 +1,7 @@
 """Host arrays of a workload that an operator would read past their end, or as another type, are refused."""
 import numpy as np
 import pytest
+import torch
 
 from paper_2312_10351_amd.runtime import Session
 from workloads import Builder
@@ -41,3 +42,17 @@ def test_arrays_have_the_size_and_type_that_is_read(dtype):
                     Session(wl, device=None)
             w[key] = values
     Session(wl, device=None)
+
+
+def test_host_arrays_of_three_axes_are_images():
+    """They are stored with their channels last, so that rows read from them would be others."""
+    b = Builder("axes", "f16")
+    b.rotary(b.ext((6, 2, 16)), 2, 16)
+    with pytest.raises(ValueError):
+        Session(b.build(1), device=None)
+    wl = b.build(1)
+    wl.ext_inputs[0] = torch.from_numpy(wl.ext_inputs[0])      # tensors are used as they are
+    Session(wl, device=None)
+    b = Builder("pixel", "f16")
+    b.gated(b.ext((32, 1, 1)), 1, 32, 8)                       # one pixel: the same in either order
+    Session(b.build(1), device=None)
