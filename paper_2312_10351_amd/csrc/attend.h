@@ -11,9 +11,10 @@
 // has too: fp16 then keeps all bits of weights down to 2^-25 of a row's largest, and below that multiples of 2^-35 of
 // it.  (Without it weights below 2^-25 of the largest were lost, which a tail of 2^16 keys and more shows.)
 // What the rounding takes off a probability is an fp16 number too (but for 2^-20 of the probability), and a second
-// product adds it where bytes and latencies are the bound, in the rows kernels: a result is then off by its own rounding alone (1500 keys, root mean square
-// against 64 bits 2.0e-4, without it 2.7e-4; 12 heads of 64 7.2 -> 7.6 us, 65536 keys 55.4 us either way).  In the
-// wide kernel, which the matrix cores bound, it is left out: causal, 8192 rows 543 us at 2.5e-4, with it 730 at 1.9e-4.
+// product adds it where bytes and latencies are the bound, in the rows kernels: a result is then off by its own
+// rounding alone (1500 keys, root mean square against 64 bits 2.0e-4, without it 2.7e-4; 12 heads of 64 7.2 -> 7.6 us,
+// 65536 keys 55.4 us either way).  In the wide kernel, which the matrix cores bound, it is left out: causal, 8192 rows
+// 543 us at 2.5e-4, with it 730 at 1.9e-4.
 //
 // rows kernels: sixteen query rows per workgroup, keys dealt to its four (deep: eight) wavefronts in tiles of KT;
 // each wavefront has its own ring in workgroup memory and its own maximum, sum and result, which meet at
@@ -478,7 +479,7 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
     const unsigned char *W = ring + TILE;
     V pf, rest;
 #pragma unroll
-    for (int e = 0; e < VE; e += 2) {
+    for (int e = 0; e < VE; e += 2) {                       // fp32: as they are
       if constexpr (ES == 2) split_probabilities(p[e / 4][e % 4], p[e / 4][e % 4 + 1], (uint32_t *)&pf + e / 2, (uint32_t *)&rest + e / 2);
       else { pf[e] = p[e / 4][e % 4]; pf[e + 1] = p[e / 4][e % 4 + 1]; }
     }
@@ -582,9 +583,10 @@ __device__ __forceinline__ void attend_rows_body(const AR &a, const Blk &b, unsi
 // a width of 128; exponentials take a quarter of the rate) and 16 KB of fragment reads each for keys and values; two
 // wavefronts per SIMD overlap the three, the one at a product first (s_setprio).  16 x 16 matrix instructions:
 // with 32 x 32 ones, which need half as many reductions, the same kernel measured 9 % slower.
-// Measured, fp16, 32 heads over 8 of 128, 8192 rows (us): causal 543 among other work (1010 TFLOP/s), 568 to 575 launched
-// back to back, all keys 1046 (1051; a large matrix product reaches 1350); 16 heads of 64, 4096 rows 88 (779).  Matrix cores busy 49 % of the
-// compute units' cycles (causal), 256 vector instructions for 64 matrix instructions of 16 cycles.
+// Measured, fp16, 32 heads over 8 of 128, 8192 rows (us): causal 543 among other work (1010 TFLOP/s), 568 to 575
+// launched back to back, all keys 1046 (1051; a large matrix product reaches 1350); 16 heads of 64, 4096 rows 88 (779).
+// Matrix cores busy 49 % of the compute units' cycles (causal), 256 vector instructions for 64 matrix instructions of
+// 16 cycles.
 constexpr int lds_attend_wide(int dp) { return 4 * 64 * dp * 2; }
 
 template <int DP, int NW, typename AR>
